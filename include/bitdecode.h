@@ -339,6 +339,111 @@ bd_status bd_paged_counted_step_lazy(const bd_paged_counted* c, const void* k_ne
                                      const void* q, float softmax_scale, int32_t num_splits,
                                      void* workspace, void* out, void* stream);
 
+/* ---- Paged cache in 8 bits, one scale per block of 128 tokens and KV head -------------------
+ *
+ * A page is a block of 128 tokens, as above, in signed 8-bit integers or in e4m3: page block_table[b][n]
+ * holds tokens 128 n .. 128 n + 127 of sequence b, and what is left behind the last whole block stays in
+ * the element type in the sequence's residual.  P = num_pages, H = n_kv_heads, D = head_dim (64 or 128):
+ *
+ *   k_codes  8 bit [P][H][128 tokens][D]       v_codes  8 bit [P][H][D][128 tokens]
+ *   k_scales fp32  [P][H]                      v_scales fp32  [P][H]           a code stands for code * scale
+ *   k_res, v_res   [B][H][128][D]              fp16 or bf16 (elem_type)
+ *   block_table    int32 [B][max_pages_per_seq]
+ *   seq_lens       int32 [B]                   tokens of every sequence BEFORE the step (>= 0)
+ *   status         int32 [1], may be NULL
+ *
+ *   Quantizer: scale = max|x| / 127 (e4m3: / 448), one fp32 division; code = x / scale in one fp32 division,
+ *   rounded to the nearest code, ties to even; zeros where the scale is 0.
+ *
+ * Calls.  A step brings rows cu_tokens[b] .. cu_tokens[b + 1] - 1 of its tensors to sequence b, one row a token, in
+ * order (cu_tokens: device int32 [B + 1]; NULL: row b is the one token of sequence b).  `total` rows are there; rows
+ * before cu_tokens[0] and from cu_tokens[B] on belong to nobody: they are not used, and of outputs left as they were.
+ * No sequence has more than max_tokens of them.  bd_paged8_append files a step's keys and values, bd_paged8_attn attends the
+ * tokens from before the step and the step's own, and bd_paged8_advance, once all is done, counts them into seq_lens: nothing
+ * else writes seq_lens or block_table, so the layers of a model can share both, and a call can be repeated.  (The first
+ * of a sequence's tokens may go to the residual rows of a block that the same step completes: a repeated
+ * bd_paged8_append gives the same cache unless a sequence whose length is no multiple of 128 crosses a block's end and
+ * stops behind it.)  What an attention call's queries are, the tokens of the step, are the newest of the cache.
+ *
+ * The host cannot check what is on the device; the kernels do, and set bits of *status: a block whose table entry is missing
+ * or not in [0, num_pages) is not read (bit 0: its tokens are not seen) or not written (bit 1); a sequence whose rows do not fit (cu_tokens
+ * out of order or beyond `total`, more than max_tokens, a negative length, one that passes 2^31 - 1) is left out, its output rows too (bit 2); a
+ * position outside of the rotation's table is taken as the nearest in it (bit 3). */
+typedef enum { BD_CODE_INT8 = 0, BD_CODE_E4M3 = 1 } bd_code_type;
+typedef enum { BD_ELEM_F16 = 0, BD_ELEM_BF16 = 1 } bd_elem_type;
+
+typedef struct bd_paged8_cache {
+  int32_t batch;
+  int32_t n_q_heads;           /* multiple of n_kv_heads */
+  int32_t n_kv_heads;
+  int32_t head_dim;            /* 64 or 128 */
+  int32_t code_type;           /* bd_code_type */
+  int32_t elem_type;           /* bd_elem_type of the residual and of every q, k, v and out */
+  int32_t num_pages;
+  int32_t max_pages_per_seq;
+  void *k_codes, *v_codes;
+  float *k_scales, *v_scales;
+  void *k_res, *v_res;
+  int32_t* block_table;
+  int32_t* seq_lens;
+  int32_t* status;
+} bd_paged8_cache;
+
+/* Rows of a step's tensor: channel d of head h of row t is element t * token_stride + h * head_stride + d of `data`
+ * (device, 16-byte aligned; strides in elements, multiples of 8, not negative).  So q, k and v may be parts of one projection's output. */
+typedef struct bd_rows {
+  void* data;
+  int64_t token_stride, head_stride;
+} bd_rows;
+
+/* Position rotation of the first rotary_dim channels (a multiple of 16, at most head_dim) of q and k: the pair (x, y) becomes
+ * (x cos - y sin, x sin + y cos), each rounded to fp32 once and then to the element type.  Pair i is channels i and
+ * i + rotary_dim / 2, or, interleaved, 2 i and 2 i + 1. */
+typedef struct bd_rotation {
+  const float* cos_sin;        /* device, 16-byte aligned, [n_positions][rotary_dim]: of a position the cosines of the rotary_dim / 2 pairs, then the sines */
+  const int32_t* positions;    /* device [total], position of every row; NULL: its index in the sequence */
+  int32_t n_positions;
+  int32_t rotary_dim;
+  int32_t interleaved;         /* 0 or 1 */
+} bd_rotation;
+
+/* What is done to the scores: s_j = softmax_scale q.k_j, then softcap * tanh(s_j / softcap) if softcap > 0, then less
+ * slopes[head] * |p - j| if there are slopes (p the query's index in its sequence, j the key's).  The query sees
+ * j < prefix_lens[b] (a prefix that every token of the sequence sees whole, also those inside of it), and j <= p with p - j < window
+ * (window 0: all of them).  A query that sees nothing gives zeros. */
+typedef struct bd_scores {
+  float softmax_scale;
+  float softcap;               /* 0: none */
+  const float* slopes;         /* device fp32 [n_q_heads], may be NULL */
+  const int32_t* prefix_lens;  /* device [B], may be NULL; one that is longer than the sequence ends with it */
+  int32_t window;
+} bd_scores;
+
+/* Size in bytes of buffer `which` (0 k_codes, 1 v_codes, 2 k_scales, 3 v_scales, 4 k_res, 5 v_res, 6 block_table, 7 seq_lens). */
+size_t bd_paged8_cache_bytes(const bd_paged8_cache* c, int which);
+
+/* Files the step's k_new, v_new ([total][H][D] as bd_rows) behind what the sequences hold: keys rotated (rot NULL: as they are), blocks that
+ * become whole quantized into their pages, the rest into the residual.  The bytes do not depend on how the tokens are shared out over
+ * calls.  q (may be NULL, or needs rot): rotated alike into q_out ([total][n_q_heads][D]), which may be q itself. */
+bd_status bd_paged8_append(const bd_paged8_cache* c, const bd_rows* k_new, const bd_rows* v_new, const bd_rows* q, const bd_rows* q_out,
+                           const int32_t* cu_tokens, int32_t total, int32_t max_tokens, const bd_rotation* rot, void* stream);
+
+/* Splits that the library would take for sequences of up to max_len tokens, the step's among them: how many workgroups
+ * share the context of a query's head group. */
+int32_t bd_paged8_choose_splits(const bd_paged8_cache* c, int32_t max_tokens, int32_t max_len);
+
+/* Bytes of device workspace that bd_paged8_attn needs for `total` rows in num_splits splits (0 for one). */
+size_t bd_paged8_workspace_bytes(const bd_paged8_cache* c, int32_t total, int32_t num_splits);
+
+/* Attention of the step's queries over the cache, after bd_paged8_append has filed the step's tokens: out (device, 16-byte aligned,
+ * [total][n_q_heads][D]) = softmax(scores) V for each row and head; query head h reads KV head h / (n_q_heads / n_kv_heads).
+ * Any num_splits >= 1 gives the same up to the rounding of fp32 sums; workspace: 16-byte aligned, may be NULL for one split. */
+bd_status bd_paged8_attn(const bd_paged8_cache* c, const bd_rows* q, const int32_t* cu_tokens, int32_t total, int32_t max_tokens,
+                         const bd_scores* scores, int32_t num_splits, void* workspace, void* out, void* stream);
+
+/* Ends a step: seq_lens[b] grows by the sequence's rows. */
+bd_status bd_paged8_advance(const bd_paged8_cache* c, const int32_t* cu_tokens, int32_t total, int32_t max_tokens, void* stream);
+
 /* Text for a status code (static storage). */
 const char* bd_strerror(bd_status s);
 

@@ -21,6 +21,9 @@ BLOCK = 128
 BD_OUT_HALF, BD_OUT_F32 = 0, 1
 BD_STATIC_SCRATCH_BYTES = 4 << 20   # include/bitdecode.h
 BD_STEP_COUNTER_BYTES = 1088
+BD_CODE_INT8, BD_CODE_E4M3 = 0, 1
+BD_ELEM_F16, BD_ELEM_BF16 = 0, 1
+CODE_TYPES = {"int8": BD_CODE_INT8, "e4m3": BD_CODE_E4M3}
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libbitdecode.so")
 _lib = None
@@ -53,6 +56,32 @@ class bd_paged_cache(ctypes.Structure):
 
 class bd_paged_counted(bd_paged_cache):
     _fields_ = [("counters", ctypes.c_void_p)]
+
+
+class bd_paged8_cache(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("code_type", ctypes.c_int32), ("elem_type", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
+        ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+        ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+        ("k_res", ctypes.c_void_p), ("v_res", ctypes.c_void_p),
+        ("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("status", ctypes.c_void_p),
+    ]
+
+
+class bd_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class bd_rotation(ctypes.Structure):
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("n_positions", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class bd_scores(ctypes.Structure):
+    _fields_ = [("softmax_scale", ctypes.c_float), ("softcap", ctypes.c_float), ("slopes", ctypes.c_void_p),
+                ("prefix_lens", ctypes.c_void_p), ("window", ctypes.c_int32)]
 
 
 class BitDecodeError(RuntimeError):
@@ -96,6 +125,13 @@ def lib() -> ctypes.CDLL:
         PC = ctypes.POINTER(bd_paged_counted)
         L.bd_paged_counted_step.restype, L.bd_paged_counted_step.argtypes = ctypes.c_int, [PC, V, V, V, F, I, V, V, V]
         L.bd_paged_counted_step_lazy.restype, L.bd_paged_counted_step_lazy.argtypes = ctypes.c_int, [PC, V, V, V, F, I, V, V, V]
+        P8, PR, PT, PS = (ctypes.POINTER(s) for s in (bd_paged8_cache, bd_rows, bd_rotation, bd_scores))
+        L.bd_paged8_cache_bytes.restype, L.bd_paged8_cache_bytes.argtypes = S, [P8, ctypes.c_int]
+        L.bd_paged8_append.restype, L.bd_paged8_append.argtypes = ctypes.c_int, [P8, PR, PR, PR, PR, V, I, I, PT, V]
+        L.bd_paged8_choose_splits.restype, L.bd_paged8_choose_splits.argtypes = I, [P8, I, I]
+        L.bd_paged8_workspace_bytes.restype, L.bd_paged8_workspace_bytes.argtypes = S, [P8, I, I]
+        L.bd_paged8_attn.restype, L.bd_paged8_attn.argtypes = ctypes.c_int, [P8, PR, V, I, I, PS, I, V, V, V]
+        L.bd_paged8_advance.restype, L.bd_paged8_advance.argtypes = ctypes.c_int, [P8, V, I, I, V]
         L.bd_strerror.restype, L.bd_strerror.argtypes = ctypes.c_char_p, [ctypes.c_int]
         L.bd_last_hip_error.restype, L.bd_last_hip_error.argtypes = ctypes.c_int, []
         _entry.update((name, ctypes.cast(getattr(L, name), V).value) for name in EXPORTS)
@@ -107,7 +143,8 @@ EXPORTS = ["bd_cache_bytes", "bd_choose_splits", "bd_step_splits", "bd_workspace
            "bd_decode_attn", "bd_decode_attn_static", "bd_probe_stream_read", "bd_decode_step", "bd_decode_step_lazy", "bd_splitk_combine", "bd_strerror", "bd_last_hip_error",
            "bd_paged_cache_bytes", "bd_paged_workspace_bytes", "bd_paged_quant_pack_kv", "bd_paged_append_kv",
            "bd_paged_decode_attn", "bd_paged_decode_step", "bd_paged_decode_step_lazy", "bd_paged_counted_step",
-           "bd_paged_counted_step_lazy"]
+           "bd_paged_counted_step_lazy", "bd_paged8_cache_bytes", "bd_paged8_append", "bd_paged8_choose_splits",
+           "bd_paged8_workspace_bytes", "bd_paged8_attn", "bd_paged8_advance"]
 
 
 def _ptr(t):
@@ -300,6 +337,44 @@ def bd_paged_decode_step_lazy(c: bd_paged_cache, k_new, v_new, q, softmax_scale:
            "bd_paged_decode_step_lazy")
 
 
+def _rows(t):
+    """bd_rows of a tensor [rows][heads][channels], or None."""
+    return None if t is None else ctypes.byref(bd_rows(t.data_ptr(), t.stride(0), t.stride(1)))
+
+
+def _ref(s):
+    return None if s is None else ctypes.byref(s)
+
+
+def bd_paged8_cache_bytes(c: bd_paged8_cache, which: int) -> int:
+    return int(lib().bd_paged8_cache_bytes(ctypes.byref(c), which))
+
+
+def bd_paged8_append(c: bd_paged8_cache, k_new, v_new, q, q_out, cu_tokens, total: int, max_tokens: int,
+                     rotation: bd_rotation | None, stream=None):
+    """k_new, v_new, q, q_out: tensors [total][heads][head_dim], channels adjacent."""
+    _check(lib().bd_paged8_append(ctypes.byref(c), _rows(k_new), _rows(v_new), _rows(q), _rows(q_out), _ptr(cu_tokens), total,
+                                  max_tokens, _ref(rotation), _stream(stream)), "bd_paged8_append")
+
+
+def bd_paged8_choose_splits(c: bd_paged8_cache, max_tokens: int, max_len: int) -> int:
+    return int(lib().bd_paged8_choose_splits(ctypes.byref(c), max_tokens, max_len))
+
+
+def bd_paged8_workspace_bytes(c: bd_paged8_cache, total: int, num_splits: int) -> int:
+    return int(lib().bd_paged8_workspace_bytes(ctypes.byref(c), total, num_splits))
+
+
+def bd_paged8_attn(c: bd_paged8_cache, q, cu_tokens, total: int, max_tokens: int, scores: bd_scores, num_splits: int, workspace,
+                   out, stream=None):
+    _check(lib().bd_paged8_attn(ctypes.byref(c), _rows(q), _ptr(cu_tokens), total, max_tokens, _ref(scores), num_splits,
+                                _ptr(workspace), _ptr(out), _stream(stream)), "bd_paged8_attn")
+
+
+def bd_paged8_advance(c: bd_paged8_cache, cu_tokens, total: int, max_tokens: int, stream=None):
+    _check(lib().bd_paged8_advance(ctypes.byref(c), _ptr(cu_tokens), total, max_tokens, _stream(stream)), "bd_paged8_advance")
+
+
 # ---- device-memory plumbing ------------------------------------------------------------------
 
 class KVCache:
@@ -459,3 +534,138 @@ class PagedKVCache:
 
     def host_buffer(self, i: int):
         return self.buffers[i][:self.sizes[i]].cpu().numpy()
+
+
+class Rotation:
+    """A position rotation: the table [positions][rotary_dim] (fp32; of a position the cosines of the rotary_dim / 2 pairs, then
+    the sines), which pairs it turns (channels i and i + rotary_dim / 2, or, interleaved, 2 i and 2 i + 1), and, if not their
+    index in the sequence, the positions of a step's rows (int32 [rows])."""
+
+    def __init__(self, cos_sin, interleaved: bool = False, positions=None):
+        import torch
+        if cos_sin.dim() != 2 or cos_sin.dtype != torch.float32 or not cos_sin.is_contiguous():
+            raise ValueError("cos_sin: a contiguous fp32 tensor [positions][rotary_dim]")
+        if positions is not None and (positions.dim() != 1 or positions.dtype != torch.int32 or not positions.is_contiguous()
+                                      or positions.device != cos_sin.device):
+            raise ValueError("positions: a contiguous int32 tensor, one for each row")
+        self.cos_sin, self.positions = cos_sin, positions
+        self.desc = bd_rotation(cos_sin.data_ptr(), _ptr(positions), cos_sin.shape[0], cos_sin.shape[1], int(interleaved))
+
+    @staticmethod
+    def table(n_positions: int, rotary_dim: int, base: float = 10000.0, device="cuda:0"):
+        """The plain table: pair i of position p turns by p * base^(-2 i / rotary_dim); angles in 64 bits."""
+        import torch
+        i = torch.arange(rotary_dim // 2, dtype=torch.float64, device=device)
+        angle = torch.arange(n_positions, dtype=torch.float64, device=device)[:, None] * base ** (-2.0 * i / rotary_dim)
+        return torch.cat([angle.cos(), angle.sin()], 1).float()
+
+
+class PagedKV8Cache:
+    """One layer's paged cache in 8 bits (one scale per block of 128 tokens and KV head): the page pool and the residuals as
+    torch tensors (zero-filled, or `buffers`, the caller's own: k_codes, v_codes, k_scales, v_scales, k_res, v_res), and the block
+    table and the lengths, which the caller owns and layers may share.  A step is append (keys and values, rotated on the way), attn
+    (any number of times) and, once for all layers that share the lengths, advance; cu_tokens (int32 [batch + 1]) says which rows of a step's
+    tensors are whose, None: row b is the one token of sequence b.  Every operation is a call into the library."""
+
+    def __init__(self, batch: int, n_q_heads: int, n_kv_heads: int, code: str, num_pages: int, block_table, head_dim: int = 128,
+                 dtype=None, seq_lens=None, buffers=None, device="cuda:0"):
+        import torch
+        elems = {torch.float16: BD_ELEM_F16, torch.bfloat16: BD_ELEM_BF16}
+        self.dtype = torch.float16 if dtype is None else dtype
+        if code not in CODE_TYPES or self.dtype not in elems:
+            raise ValueError(f"code: {', '.join(CODE_TYPES)}; dtype: torch.float16 or torch.bfloat16")
+        self.code, self.device = code, torch.device(device)
+        self.block_table = torch.as_tensor(block_table, dtype=torch.int32).contiguous().to(device)
+        if self.block_table.dim() != 2 or self.block_table.shape[0] != batch:
+            raise ValueError("block_table: [batch][pages of a sequence]")
+        self.desc = bd_paged8_cache(batch, n_q_heads, n_kv_heads, head_dim, CODE_TYPES[code], elems[self.dtype], num_pages,
+                                    self.block_table.shape[1])
+        self.sizes = [bd_paged8_cache_bytes(self.desc, i) for i in range(8)]
+        if self.sizes[0] == 0:
+            raise BitDecodeError(-1, "bd_paged8_cache_bytes")
+        if buffers is None:
+            buffers = [torch.zeros(n, dtype=torch.uint8, device=device) for n in self.sizes[:6]]
+        for t, n in zip(buffers, self.sizes, strict=False):
+            if t.numel() * t.element_size() != n or not t.is_contiguous() or t.device != self.block_table.device:
+                raise ValueError(f"buffers: contiguous tensors of {self.sizes[:6]} bytes on {self.block_table.device}")
+        self.buffers = list(buffers)
+        self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.k_res, self.v_res = self.buffers
+        self.seq_lens = torch.zeros(batch, dtype=torch.int32, device=device) if seq_lens is None else seq_lens
+        if self.seq_lens.dtype != torch.int32 or tuple(self.seq_lens.shape) != (batch,) or not self.seq_lens.is_contiguous() \
+                or self.seq_lens.device != self.block_table.device:
+            raise ValueError(f"seq_lens: a contiguous int32 tensor [batch] on {self.block_table.device}")
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        for name, buf in zip(["k_codes", "v_codes", "k_scales", "v_scales", "k_res", "v_res", "block_table", "seq_lens", "status"],
+                             self.buffers + [self.block_table, self.seq_lens, self.status]):
+            setattr(self.desc, name, buf.data_ptr())
+        self.max_len = (self.desc.max_pages_per_seq + 1) * BLOCK - 1   # tokens that a sequence can have
+        self._ws = None
+        self._retired = []
+
+    def _rows_of(self, t, heads: int, what: str) -> int:
+        """Checks a step's tensor; its rows."""
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.desc.head_dim or t.dtype != self.dtype or t.stride(2) != 1 \
+                or t.device != self.block_table.device:
+            raise ValueError(f"{what}: a {self.dtype} tensor [rows][{heads}][{self.desc.head_dim}] on {self.block_table.device}, channels adjacent")
+        return t.shape[0]
+
+    def _list(self, t, n: int, dtype_name: str, what: str):
+        if t is not None and (str(t.dtype) != "torch." + dtype_name or tuple(t.shape) != (n,) or not t.is_contiguous()
+                              or t.device != self.block_table.device):
+            raise ValueError(f"{what}: a contiguous {dtype_name} tensor [{n}] on {self.block_table.device}")
+        return t
+
+    def append(self, k_new, v_new, q=None, q_out=None, cu_tokens=None, max_tokens: int = 1, rotation: Rotation | None = None, stream=None):
+        """Files the step's keys and values; q, if given, is rotated into q_out (may be q itself), which is returned."""
+        rows = self._rows_of(k_new, self.desc.n_kv_heads, "k_new")
+        same = self._rows_of(v_new, self.desc.n_kv_heads, "v_new") == rows
+        if q is not None:
+            if q_out is None:
+                raise ValueError("q needs q_out")
+            same = same and self._rows_of(q, self.desc.n_q_heads, "q") == rows == self._rows_of(q_out, self.desc.n_q_heads, "q_out")
+        if not same:
+            raise ValueError("k_new, v_new, q and q_out have one row for each token")
+        if rotation is not None:
+            if rotation.cos_sin.device != self.block_table.device:
+                raise ValueError(f"rotation: on {self.block_table.device}")
+            self._list(rotation.positions, rows, "int32", "positions")
+        self._list(cu_tokens, self.desc.batch + 1, "int32", "cu_tokens")
+        bd_paged8_append(self.desc, k_new, v_new, q, None if q is None else q_out, cu_tokens, rows, max_tokens,
+                         None if rotation is None else rotation.desc, stream)
+        return q_out
+
+    def workspace(self, rows: int, num_splits: int):
+        """As KVCache.workspace: grows only, outgrown buffers stay alive."""
+        need = bd_paged8_workspace_bytes(self.desc, rows, num_splits)
+        if self._ws is None or self._ws.numel() < need:
+            import torch
+            if self._ws is not None:
+                self._retired.append(self._ws)
+            self._ws = torch.empty(max(need, 16), dtype=torch.uint8, device=self.device)
+        return self._ws
+
+    def attn(self, q, softmax_scale: float, out, cu_tokens=None, max_tokens: int = 1, max_len: int | None = None, softcap: float = 0.0,
+             slopes=None, window: int = 0, prefix_lens=None, num_splits: int | None = None, stream=None):
+        """Attention of the step's queries into out [rows][n_q_heads][head_dim].  max_len: the longest sequence's tokens, the step's among
+        them, which num_splits is chosen for (any value gives the same result)."""
+        rows = self._rows_of(q, self.desc.n_q_heads, "q")
+        if self._rows_of(out, self.desc.n_q_heads, "out") != rows or not out.is_contiguous():
+            raise ValueError("out: contiguous, a row for each of q")
+        self._list(cu_tokens, self.desc.batch + 1, "int32", "cu_tokens")
+        self._list(slopes, self.desc.n_q_heads, "float32", "slopes")
+        self._list(prefix_lens, self.desc.batch, "int32", "prefix_lens")
+        if num_splits is None:
+            num_splits = bd_paged8_choose_splits(self.desc, max_tokens, self.max_len if max_len is None else max_len)
+        ws = None if num_splits == 1 else self.workspace(rows, num_splits)
+        bd_paged8_attn(self.desc, q, cu_tokens, rows, max_tokens, bd_scores(softmax_scale, softcap, _ptr(slopes), _ptr(prefix_lens), window),
+                       num_splits, ws, out, stream)
+        return out
+
+    def advance(self, cu_tokens=None, rows: int | None = None, max_tokens: int = 1, stream=None):
+        """Counts the step's tokens into seq_lens.  rows: of the step's tensors (of one token a sequence, the batch)."""
+        self._list(cu_tokens, self.desc.batch + 1, "int32", "cu_tokens")
+        bd_paged8_advance(self.desc, cu_tokens, self.desc.batch if rows is None else rows, max_tokens, stream)
+
+    def host_buffer(self, i: int):
+        import torch
+        return self.buffers[i].flatten().view(torch.uint8).cpu().numpy()

@@ -8,7 +8,8 @@ import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = ["bd_api.hip", "bd_quant.hip", "bd_decode.hip", "bd_decode_mx.hip", "bd_decode_grp.hip"]
+SOURCES = ["bd_api.hip", "bd_quant.hip", "bd_decode.hip", "bd_decode_mx.hip", "bd_decode_grp.hip",
+           "bd_kv8_append.hip", "bd_kv8_few.hip", "bd_kv8_many.hip", "bd_kv8_api.hip"]
 LIB = os.path.join(HERE, "libbitdecode.so")
 
 FLAGS = [
