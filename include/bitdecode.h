@@ -432,8 +432,11 @@ bd_status bd_paged8_append(const bd_paged8_cache* c, const bd_rows* k_new, const
  * share the context of a query's head group. */
 int32_t bd_paged8_choose_splits(const bd_paged8_cache* c, int32_t max_tokens, int32_t max_len);
 
-/* Bytes of device workspace that bd_paged8_attn needs for `total` rows in num_splits splits (0 for one). */
-size_t bd_paged8_workspace_bytes(const bd_paged8_cache* c, int32_t total, int32_t num_splits);
+/* Bytes of device workspace that bd_paged8_attn needs for a step of `total` rows, up to max_tokens of a sequence, in num_splits splits (0 for
+ * one).  Its first BD_PAGED8_COUNTER_BYTES are counters: zeros before the first call that is given the workspace, and every call leaves them as
+ * zeros.  Calls that may overlap need workspaces of their own. */
+#define BD_PAGED8_COUNTER_BYTES 65536
+size_t bd_paged8_workspace_bytes(const bd_paged8_cache* c, int32_t total, int32_t max_tokens, int32_t num_splits);
 
 /* Attention of the step's queries over the cache, after bd_paged8_append has filed the step's tokens: out (device, 16-byte aligned,
  * [total][n_q_heads][D]) = softmax(scores) V for each row and head; query head h reads KV head h / (n_q_heads / n_kv_heads).

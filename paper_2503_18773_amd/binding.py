@@ -129,7 +129,7 @@ def lib() -> ctypes.CDLL:
         L.bd_paged8_cache_bytes.restype, L.bd_paged8_cache_bytes.argtypes = S, [P8, ctypes.c_int]
         L.bd_paged8_append.restype, L.bd_paged8_append.argtypes = ctypes.c_int, [P8, PR, PR, PR, PR, V, I, I, PT, V]
         L.bd_paged8_choose_splits.restype, L.bd_paged8_choose_splits.argtypes = I, [P8, I, I]
-        L.bd_paged8_workspace_bytes.restype, L.bd_paged8_workspace_bytes.argtypes = S, [P8, I, I]
+        L.bd_paged8_workspace_bytes.restype, L.bd_paged8_workspace_bytes.argtypes = S, [P8, I, I, I]
         L.bd_paged8_attn.restype, L.bd_paged8_attn.argtypes = ctypes.c_int, [P8, PR, V, I, I, PS, I, V, V, V]
         L.bd_paged8_advance.restype, L.bd_paged8_advance.argtypes = ctypes.c_int, [P8, V, I, I, V]
         L.bd_strerror.restype, L.bd_strerror.argtypes = ctypes.c_char_p, [ctypes.c_int]
@@ -207,6 +207,56 @@ class _CtypesCall:
         status = _CtypesCall._function(fn, ctypes.c_int, V, V, V, I, V, V, V)(
             ctypes.addressof(c), _ptr(k), _ptr(v), L, ctypes.addressof(pl), ctypes.addressof(rl), stream)
         return status, pl.value, rl.value
+
+
+    # (paged cache in 8 bits, with the checks of a step's tensors)
+    @staticmethod
+    def _rows_of(t, layout, heads, contiguous, what, rows):
+        _, _, _, dim, dtype, _, _, device, where = layout
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.dtype != dtype or t.stride(2) != 1 or t.get_device() != device \
+                or (rows is not None and t.shape[0] != rows) or (contiguous and not t.is_contiguous()):
+            raise ValueError(f"{what}: a {dtype} tensor [{'rows' if rows is None else rows}][{heads}][{dim}] on {where}, "
+                             f"{'contiguous' if contiguous else 'channels adjacent'}")
+        return bd_rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+    @staticmethod
+    def _list_of(t, layout, n, dtype, what):
+        if t is not None and (t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous() or t.get_device() != layout[7]):
+            raise ValueError(f"{what}: a contiguous {dtype} tensor [{n}] on {layout[8]}")
+        return _ptr(t)
+
+    @staticmethod
+    def append8(fn, c, layout, k_new, v_new, q, q_out, cu_tokens, max_tokens, rotation, positions, stream):
+        V, I, me = ctypes.c_void_p, ctypes.c_int32, _CtypesCall
+        k = me._rows_of(k_new, layout, layout[2], False, "k_new", None)
+        n = k_new.shape[0]
+        rows = [k, me._rows_of(v_new, layout, layout[2], False, "v_new", n), None, None]
+        if q is not None:
+            if q_out is None:
+                raise ValueError("q needs q_out")
+            rows[2:] = [me._rows_of(t, layout, layout[1], False, what, n) for t, what in ((q, "q"), (q_out, "q_out"))]
+        cu = me._list_of(cu_tokens, layout, layout[0] + 1, layout[5], "cu_tokens")
+        me._list_of(positions, layout, n, layout[5], "positions")
+        at = [None if s is None else ctypes.addressof(s) for s in rows + [rotation]]
+        return me._function(fn, ctypes.c_int, V, V, V, V, V, V, I, I, V, V)(ctypes.addressof(c), *at[:4], cu, n, max_tokens, at[4], stream)
+
+    @staticmethod
+    def plan8(choose, size, c, rows, max_tokens, max_len, num_splits):
+        V, I = ctypes.c_void_p, ctypes.c_int32
+        at = ctypes.addressof(c)
+        ns = num_splits or _CtypesCall._function(choose, I, V, I, I)(at, max_tokens, max_len)
+        return ns, _CtypesCall._function(size, ctypes.c_size_t, V, I, I, I)(at, rows, max_tokens, ns)
+
+    @staticmethod
+    def attn8(fn, c, layout, q, cu_tokens, max_tokens, scale, softcap, slopes, prefix_lens, window, num_splits, ws, out, stream):
+        V, I, me = ctypes.c_void_p, ctypes.c_int32, _CtypesCall
+        rows = me._rows_of(q, layout, layout[1], False, "q", None)
+        o = me._rows_of(out, layout, layout[1], True, "out", q.shape[0])
+        cu = me._list_of(cu_tokens, layout, layout[0] + 1, layout[5], "cu_tokens")
+        s = bd_scores(scale, softcap, me._list_of(slopes, layout, layout[1], layout[6], "slopes"),
+                      me._list_of(prefix_lens, layout, layout[0], layout[5], "prefix_lens"), window)
+        return me._function(fn, ctypes.c_int, V, V, V, I, I, V, I, V, V, V)(
+            ctypes.addressof(c), ctypes.addressof(rows), cu, q.shape[0], max_tokens, ctypes.addressof(s), num_splits, _ptr(ws), o.data, stream)
 
 
 try:
@@ -361,8 +411,8 @@ def bd_paged8_choose_splits(c: bd_paged8_cache, max_tokens: int, max_len: int) -
     return int(lib().bd_paged8_choose_splits(ctypes.byref(c), max_tokens, max_len))
 
 
-def bd_paged8_workspace_bytes(c: bd_paged8_cache, total: int, num_splits: int) -> int:
-    return int(lib().bd_paged8_workspace_bytes(ctypes.byref(c), total, num_splits))
+def bd_paged8_workspace_bytes(c: bd_paged8_cache, total: int, max_tokens: int, num_splits: int) -> int:
+    return int(lib().bd_paged8_workspace_bytes(ctypes.byref(c), total, max_tokens, num_splits))
 
 
 def bd_paged8_attn(c: bd_paged8_cache, q, cu_tokens, total: int, max_tokens: int, scores: bd_scores, num_splits: int, workspace,
@@ -548,7 +598,7 @@ class Rotation:
         if positions is not None and (positions.dim() != 1 or positions.dtype != torch.int32 or not positions.is_contiguous()
                                       or positions.device != cos_sin.device):
             raise ValueError("positions: a contiguous int32 tensor, one for each row")
-        self.cos_sin, self.positions = cos_sin, positions
+        self.cos_sin, self.positions, self.device = cos_sin, positions, cos_sin.get_device()
         self.desc = bd_rotation(cos_sin.data_ptr(), _ptr(positions), cos_sin.shape[0], cos_sin.shape[1], int(interleaved))
 
     @staticmethod
@@ -599,71 +649,48 @@ class PagedKV8Cache:
                              self.buffers + [self.block_table, self.seq_lens, self.status]):
             setattr(self.desc, name, buf.data_ptr())
         self.max_len = (self.desc.max_pages_per_seq + 1) * BLOCK - 1   # tokens that a sequence can have
-        self._ws = None
+        where = self.block_table.device
+        self._layout = (batch, n_q_heads, n_kv_heads, head_dim, self.dtype, torch.int32, torch.float32, self.block_table.get_device(), where)
+        self._ws, self._ws_bytes = None, 0
         self._retired = []
 
-    def _rows_of(self, t, heads: int, what: str) -> int:
-        """Checks a step's tensor; its rows."""
-        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.desc.head_dim or t.dtype != self.dtype or t.stride(2) != 1 \
-                or t.device != self.block_table.device:
-            raise ValueError(f"{what}: a {self.dtype} tensor [rows][{heads}][{self.desc.head_dim}] on {self.block_table.device}, channels adjacent")
-        return t.shape[0]
-
-    def _list(self, t, n: int, dtype_name: str, what: str):
-        if t is not None and (str(t.dtype) != "torch." + dtype_name or tuple(t.shape) != (n,) or not t.is_contiguous()
-                              or t.device != self.block_table.device):
-            raise ValueError(f"{what}: a contiguous {dtype_name} tensor [{n}] on {self.block_table.device}")
-        return t
-
     def append(self, k_new, v_new, q=None, q_out=None, cu_tokens=None, max_tokens: int = 1, rotation: Rotation | None = None, stream=None):
-        """Files the step's keys and values; q, if given, is rotated into q_out (may be q itself), which is returned."""
-        rows = self._rows_of(k_new, self.desc.n_kv_heads, "k_new")
-        same = self._rows_of(v_new, self.desc.n_kv_heads, "v_new") == rows
-        if q is not None:
-            if q_out is None:
-                raise ValueError("q needs q_out")
-            same = same and self._rows_of(q, self.desc.n_q_heads, "q") == rows == self._rows_of(q_out, self.desc.n_q_heads, "q_out")
-        if not same:
-            raise ValueError("k_new, v_new, q and q_out have one row for each token")
-        if rotation is not None:
-            if rotation.cos_sin.device != self.block_table.device:
-                raise ValueError(f"rotation: on {self.block_table.device}")
-            self._list(rotation.positions, rows, "int32", "positions")
-        self._list(cu_tokens, self.desc.batch + 1, "int32", "cu_tokens")
-        bd_paged8_append(self.desc, k_new, v_new, q, None if q is None else q_out, cu_tokens, rows, max_tokens,
-                         None if rotation is None else rotation.desc, stream)
+        """Files the step's keys and values; q, if given, is rotated into q_out (may be q itself), which is returned.  All of them
+        [rows][heads][head_dim] in the cache's type, channels adjacent."""
+        if rotation is None:
+            desc = positions = None
+        else:
+            desc, positions = rotation.desc, rotation.positions
+            if rotation.device != self._layout[7]:
+                raise ValueError(f"rotation: on {self._layout[8]}")
+        _check(_call.append8(_address("bd_paged8_append"), self.desc, self._layout, k_new, v_new, q, q_out, cu_tokens, max_tokens, desc,
+                             positions, _stream(stream)), "bd_paged8_append")
         return q_out
 
-    def workspace(self, rows: int, num_splits: int):
-        """As KVCache.workspace: grows only, outgrown buffers stay alive."""
-        need = bd_paged8_workspace_bytes(self.desc, rows, num_splits)
-        if self._ws is None or self._ws.numel() < need:
+    def workspace(self, rows: int, max_tokens: int, max_len: int, num_splits: int):
+        """The splits of a call (num_splits; 0: chosen for max_len) and a workspace for it, None for one split.  As KVCache.workspace
+        it grows only, and outgrown buffers stay alive."""
+        num_splits, need = _call.plan8(_address("bd_paged8_choose_splits"), _address("bd_paged8_workspace_bytes"), self.desc, rows, max_tokens,
+                                       max_len, num_splits)
+        if need > self._ws_bytes:
             import torch
             if self._ws is not None:
                 self._retired.append(self._ws)
-            self._ws = torch.empty(max(need, 16), dtype=torch.uint8, device=self.device)
-        return self._ws
+            self._ws, self._ws_bytes = torch.zeros(need, dtype=torch.uint8, device=self.device), need
+        return num_splits, self._ws if need else None
 
     def attn(self, q, softmax_scale: float, out, cu_tokens=None, max_tokens: int = 1, max_len: int | None = None, softcap: float = 0.0,
              slopes=None, window: int = 0, prefix_lens=None, num_splits: int | None = None, stream=None):
-        """Attention of the step's queries into out [rows][n_q_heads][head_dim].  max_len: the longest sequence's tokens, the step's among
-        them, which num_splits is chosen for (any value gives the same result)."""
-        rows = self._rows_of(q, self.desc.n_q_heads, "q")
-        if self._rows_of(out, self.desc.n_q_heads, "out") != rows or not out.is_contiguous():
-            raise ValueError("out: contiguous, a row for each of q")
-        self._list(cu_tokens, self.desc.batch + 1, "int32", "cu_tokens")
-        self._list(slopes, self.desc.n_q_heads, "float32", "slopes")
-        self._list(prefix_lens, self.desc.batch, "int32", "prefix_lens")
-        if num_splits is None:
-            num_splits = bd_paged8_choose_splits(self.desc, max_tokens, self.max_len if max_len is None else max_len)
-        ws = None if num_splits == 1 else self.workspace(rows, num_splits)
-        bd_paged8_attn(self.desc, q, cu_tokens, rows, max_tokens, bd_scores(softmax_scale, softcap, _ptr(slopes), _ptr(prefix_lens), window),
-                       num_splits, ws, out, stream)
+        """Attention of the step's queries into out (contiguous), both [rows][n_q_heads][head_dim].  max_len: the longest sequence's tokens,
+        the step's among them, which num_splits is chosen for (any value gives the same result)."""
+        num_splits, ws = self.workspace(len(q), max_tokens, self.max_len if max_len is None else max_len, num_splits or 0)
+        _check(_call.attn8(_address("bd_paged8_attn"), self.desc, self._layout, q, cu_tokens, max_tokens, softmax_scale, softcap, slopes,
+                           prefix_lens, window, num_splits, ws, out, _stream(stream)), "bd_paged8_attn")
         return out
 
     def advance(self, cu_tokens=None, rows: int | None = None, max_tokens: int = 1, stream=None):
         """Counts the step's tokens into seq_lens.  rows: of the step's tensors (of one token a sequence, the batch)."""
-        self._list(cu_tokens, self.desc.batch + 1, "int32", "cu_tokens")
+        _CtypesCall._list_of(cu_tokens, self._layout, self.desc.batch + 1, self._layout[5], "cu_tokens")
         bd_paged8_advance(self.desc, cu_tokens, self.desc.batch if rows is None else rows, max_tokens, stream)
 
     def host_buffer(self, i: int):

@@ -53,7 +53,7 @@ def _build_call() -> None:
     out = os.path.join(HERE, "_bdcall" + sysconfig.get_config_var("EXT_SUFFIX"))
     if os.path.exists(out):
         os.remove(out)
-    cmd = [os.environ.get("CC", "gcc"), "-O2", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"],
+    cmd = [os.environ.get("CC", "gcc"), "-O2", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"),
            os.path.join(HERE, "csrc", "bd_call.c"), "-o", out]
     try:
         res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)

@@ -11,7 +11,9 @@
 #include <Python.h>
 #include <stdint.h>
 
-static PyObject* name_data_ptr;
+#include "bitdecode.h"
+
+static PyObject *name_data_ptr, *name_shape, *name_stride, *name_dtype, *name_get_device;
 
 /* Address of a tensor's data, NULL for None; -1 with an exception set. */
 static int tensor_address(PyObject* t, void** p) {
@@ -134,16 +136,186 @@ static PyObject* quant(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   return Py_BuildValue("(iii)", status, (int)packed, (int)res);
 }
 
+/* ---- Paged cache in 8 bits.  These check the tensors too: in Python that took longer than all the rest of a call. ---- */
+
+/* PagedKV8Cache._layout: (batch, query heads, KV heads, head_dim, dtype, int32, float32, number of the device, text for the device). */
+typedef struct {
+  long batch, q_heads, kv_heads, dim, device;
+  PyObject *dtype, *int32, *float32, *where;
+} layout8;
+static int layout_of(PyObject* o, layout8* l) {
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 9) {
+    PyErr_SetString(PyExc_TypeError, "layout");
+    return -1;
+  }
+  l->batch = PyLong_AsLong(PyTuple_GET_ITEM(o, 0));
+  l->q_heads = PyLong_AsLong(PyTuple_GET_ITEM(o, 1));
+  l->kv_heads = PyLong_AsLong(PyTuple_GET_ITEM(o, 2));
+  l->dim = PyLong_AsLong(PyTuple_GET_ITEM(o, 3));
+  l->dtype = PyTuple_GET_ITEM(o, 4);
+  l->int32 = PyTuple_GET_ITEM(o, 5);
+  l->float32 = PyTuple_GET_ITEM(o, 6);
+  l->device = PyLong_AsLong(PyTuple_GET_ITEM(o, 7));
+  l->where = PyTuple_GET_ITEM(o, 8);
+  return PyErr_Occurred() ? -1 : 0;
+}
+/* Up to 3 sizes and strides of a tensor of `dims` dimensions, of the given type on the given device: 1; 0 if it is another; -1 error. */
+static int tensor_is(PyObject* t, int dims, PyObject* dtype, long device, long* size, long* stride) {
+  PyObject *shape = NULL, *strides = NULL, *type = NULL, *dev = NULL;
+  int ok = -1;
+  if (!(shape = PyObject_GetAttr(t, name_shape)) || !(strides = PyObject_CallMethodNoArgs(t, name_stride)) ||
+      !(type = PyObject_GetAttr(t, name_dtype)) || !(dev = PyObject_CallMethodNoArgs(t, name_get_device)))
+    goto out;
+  ok = 0;
+  if (!PyTuple_Check(shape) || PyTuple_GET_SIZE(shape) != dims || !PyTuple_Check(strides) || PyTuple_GET_SIZE(strides) != dims || type != dtype ||
+      PyLong_AsLong(dev) != device)
+    goto out;
+  for (int i = 0; i < dims; ++i) {
+    size[i] = PyLong_AsLong(PyTuple_GET_ITEM(shape, i));
+    stride[i] = PyLong_AsLong(PyTuple_GET_ITEM(strides, i));
+  }
+  ok = 1;
+out:
+  Py_XDECREF(shape);
+  Py_XDECREF(strides);
+  Py_XDECREF(type);
+  Py_XDECREF(dev);
+  return PyErr_Occurred() ? -1 : ok;
+}
+/* A step's tensor [rows][heads][channels]; *rows -1: whatever it has. */
+static int rows_of(PyObject* t, const layout8* l, long heads, int contiguous, const char* what, bd_rows* r, long* rows) {
+  long size[3], stride[3];
+  void* p;
+  const int ok = tensor_is(t, 3, l->dtype, l->device, size, stride);
+  if (ok < 0) return -1;
+  if (!ok || size[1] != heads || size[2] != l->dim || stride[2] != 1 || (*rows >= 0 && size[0] != *rows) ||
+      (contiguous && ((heads > 1 && stride[1] != l->dim) || (size[0] > 1 && stride[0] != heads * l->dim)))) {
+    if (*rows >= 0)
+      PyErr_Format(PyExc_ValueError, "%s: a %S tensor [%ld][%ld][%ld] on %S, %s", what, l->dtype, *rows, heads, l->dim, l->where,
+                   contiguous ? "contiguous" : "channels adjacent");
+    else
+      PyErr_Format(PyExc_ValueError, "%s: a %S tensor [rows][%ld][%ld] on %S, channels adjacent", what, l->dtype, heads, l->dim, l->where);
+    return -1;
+  }
+  if (tensor_address(t, &p)) return -1;
+  r->data = p;
+  r->token_stride = stride[0];
+  r->head_stride = stride[1];
+  *rows = size[0];
+  return 0;
+}
+/* A list of n numbers, or None. */
+static int list_of(PyObject* t, const layout8* l, long n, PyObject* dtype, const char* what, void** p) {
+  long size, stride;
+  int ok;
+  *p = NULL;
+  if (t == Py_None) return 0;
+  ok = tensor_is(t, 1, dtype, l->device, &size, &stride);
+  if (ok < 0) return -1;
+  if (!ok || size != n || (n > 1 && stride != 1)) {
+    PyErr_Format(PyExc_ValueError, "%s: a contiguous %S tensor [%ld] on %S", what, dtype, n, l->where);
+    return -1;
+  }
+  return tensor_address(t, p);
+}
+
+/* append8(fn, cache, layout, k_new, v_new, q, q_out, cu_tokens, max_tokens, rotation, positions, stream) -> status   (bd_paged8_append) */
+static PyObject* append8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void *fn, *cu, *positions, *stream;
+  layout8 l;
+  bd_rows k, v, q = {0}, q_out = {0};
+  long rows = -1;
+  int32_t most;
+  int status, has_q;
+  Py_buffer c, rot = {0};
+  (void)self;
+  if (!count_is(n, 12) || address(a[0], &fn) || layout_of(a[2], &l) || rows_of(a[3], &l, l.kv_heads, 0, "k_new", &k, &rows) ||
+      rows_of(a[4], &l, l.kv_heads, 0, "v_new", &v, &rows))
+    return NULL;
+  has_q = a[5] != Py_None;
+  if (has_q && a[6] == Py_None) {
+    PyErr_SetString(PyExc_ValueError, "q needs q_out");
+    return NULL;
+  }
+  if ((has_q && (rows_of(a[5], &l, l.q_heads, 0, "q", &q, &rows) || rows_of(a[6], &l, l.q_heads, 0, "q_out", &q_out, &rows))) ||
+      list_of(a[7], &l, l.batch + 1, l.int32, "cu_tokens", &cu) || int32_of(a[8], &most) || list_of(a[10], &l, rows, l.int32, "positions", &positions) ||
+      address(a[11], &stream) || (a[9] != Py_None && structure(a[9], &rot)))
+    return NULL;
+  if (structure(a[1], &c)) {
+    if (rot.buf) PyBuffer_Release(&rot);
+    return NULL;
+  }
+  Py_BEGIN_ALLOW_THREADS
+  status = ((int (*)(const void*, const bd_rows*, const bd_rows*, const bd_rows*, const bd_rows*, const void*, int32_t, int32_t, const void*, void*))fn)(
+      c.buf, &k, &v, has_q ? &q : NULL, has_q ? &q_out : NULL, cu, (int32_t)rows, most, rot.buf, stream);
+  Py_END_ALLOW_THREADS
+  PyBuffer_Release(&c);
+  if (rot.buf) PyBuffer_Release(&rot);
+  return PyLong_FromLong(status);
+}
+
+/* plan8(choose, bytes, cache, rows, max_tokens, max_len, num_splits) -> (num_splits, workspace bytes)
+ *   (bd_paged8_choose_splits where num_splits is 0, bd_paged8_workspace_bytes) */
+static PyObject* plan8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void *choose, *bytes;
+  int32_t rows, most, len, ns;
+  size_t need;
+  Py_buffer c;
+  (void)self;
+  if (!count_is(n, 7) || address(a[0], &choose) || address(a[1], &bytes) || int32_of(a[3], &rows) || int32_of(a[4], &most) ||
+      int32_of(a[5], &len) || int32_of(a[6], &ns) || structure(a[2], &c))
+    return NULL;
+  if (!ns) ns = ((int32_t(*)(const void*, int32_t, int32_t))choose)(c.buf, most, len);
+  need = ((size_t(*)(const void*, int32_t, int32_t, int32_t))bytes)(c.buf, rows, most, ns);
+  PyBuffer_Release(&c);
+  return Py_BuildValue("(in)", (int)ns, (Py_ssize_t)need);
+}
+
+/* attn8(fn, cache, layout, q, cu_tokens, max_tokens, scale, softcap, slopes, prefix_lens, window, num_splits, workspace, out, stream) -> status
+ *   (bd_paged8_attn) */
+static PyObject* attn8(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  void *fn, *cu, *slopes, *prefix, *ws, *stream;
+  layout8 l;
+  bd_rows q, out;
+  bd_scores s;
+  long rows = -1;
+  int32_t most, ns;
+  int status;
+  Py_buffer c;
+  (void)self;
+  if (!count_is(n, 15) || address(a[0], &fn) || layout_of(a[2], &l) || rows_of(a[3], &l, l.q_heads, 0, "q", &q, &rows) ||
+      rows_of(a[13], &l, l.q_heads, 1, "out", &out, &rows) || list_of(a[4], &l, l.batch + 1, l.int32, "cu_tokens", &cu) || int32_of(a[5], &most) ||
+      float_of(a[6], &s.softmax_scale) || float_of(a[7], &s.softcap) || list_of(a[8], &l, l.q_heads, l.float32, "slopes", &slopes) ||
+      list_of(a[9], &l, l.batch, l.int32, "prefix_lens", &prefix) || int32_of(a[10], &s.window) || int32_of(a[11], &ns) || tensor_address(a[12], &ws) ||
+      address(a[14], &stream) || structure(a[1], &c))
+    return NULL;
+  s.slopes = slopes;
+  s.prefix_lens = prefix;
+  Py_BEGIN_ALLOW_THREADS
+  status = ((int (*)(const void*, const bd_rows*, const void*, int32_t, int32_t, const bd_scores*, int32_t, void*, void*, void*))fn)(
+      c.buf, &q, cu, (int32_t)rows, most, &s, ns, ws, out.data, stream);
+  Py_END_ALLOW_THREADS
+  PyBuffer_Release(&c);
+  return PyLong_FromLong(status);
+}
+
 static PyMethodDef methods[] = {
     {"splits", (PyCFunction)(void (*)(void))splits, METH_FASTCALL, NULL},
     {"step", (PyCFunction)(void (*)(void))step, METH_FASTCALL, NULL},
     {"paged_step", (PyCFunction)(void (*)(void))paged_step, METH_FASTCALL, NULL},
     {"paged_quant", (PyCFunction)(void (*)(void))paged_quant, METH_FASTCALL, NULL},
     {"quant", (PyCFunction)(void (*)(void))quant, METH_FASTCALL, NULL},
+    {"append8", (PyCFunction)(void (*)(void))append8, METH_FASTCALL, NULL},
+    {"plan8", (PyCFunction)(void (*)(void))plan8, METH_FASTCALL, NULL},
+    {"attn8", (PyCFunction)(void (*)(void))attn8, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bdcall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__bdcall(void) {
   name_data_ptr = PyUnicode_InternFromString("data_ptr");
-  return name_data_ptr ? PyModule_Create(&module) : NULL;
+  name_shape = PyUnicode_InternFromString("shape");
+  name_stride = PyUnicode_InternFromString("stride");
+  name_dtype = PyUnicode_InternFromString("dtype");
+  name_get_device = PyUnicode_InternFromString("get_device");
+  return name_data_ptr && name_shape && name_stride && name_dtype && name_get_device ? PyModule_Create(&module) : NULL;
 }

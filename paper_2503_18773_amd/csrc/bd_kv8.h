@@ -38,7 +38,7 @@ struct Scores8 {
 hipError_t launch_kv8_append(const Step8& s, int head_dim, int code, int elem, const Rows8& k, const Rows8& v, const Rows8& q,
                              const Rows8& q_out, const Rotate8& rot, hipStream_t st);
 hipError_t launch_kv8_advance(const Step8& s, hipStream_t st);
-hipError_t launch_kv8_attn(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, float* part,
+hipError_t launch_kv8_attn(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, void* ws,
                            void* out, hipStream_t st);
 int kv8_splits(const bd_paged8_cache* c, int max_tokens, int max_len);
 
@@ -49,10 +49,14 @@ namespace {
 struct Seq8 {
   int len, row, n;   // tokens before the step, first row, rows
 };
-__device__ __forceinline__ bool step_rows(const Step8& s, int b, Seq8& q, bool every_thread = false) {
-  q.len = s.seq_lens[b];
-  q.row = s.cu ? s.cu[b] : b;
-  const int end = s.cu ? s.cu[b + 1] : b + 1;
+struct PlainLoad {
+  __device__ __forceinline__ int32_t operator()(const int32_t* p) const { return *p; }
+};
+template <class Load = PlainLoad>
+__device__ __forceinline__ bool step_rows(const Step8& s, int b, Seq8& q, bool every_thread = false, Load load = Load()) {
+  q.len = load(s.seq_lens + b);
+  q.row = s.cu ? load(s.cu + b) : b;
+  const int end = s.cu ? load(s.cu + b + 1) : b + 1;
   const bool rows = q.row >= 0 && end >= q.row && end <= s.total;
   q.n = rows ? end - q.row : 0;
   const bool fits = rows && q.n <= s.max_tokens && q.len >= 0 && q.len <= 0x7fffffff - q.n;

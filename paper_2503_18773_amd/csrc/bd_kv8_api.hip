@@ -11,7 +11,7 @@ template <int D, int ELEM>
 __global__ __launch_bounds__(256) void kv8_merge_kernel(Step8 s, int splits, const float* part, uint16_t* out) {
   const int b = blockIdx.y, lane = threadIdx.x & 63;
   Seq8 sq;
-  if (!step_rows(s, b, sq)) return;
+  if (!queries_of(s, b, sq)) return;
   const long i = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (i >= (long)sq.n * s.n_q_heads) return;
   const size_t rows = (size_t)s.total * s.n_q_heads, row = (size_t)sq.row * s.n_q_heads + i;
@@ -112,17 +112,27 @@ constexpr long kFewRows = 64;
 
 bool kv8_few(long rows) { return rows <= kFewRows; }
 
+// Few rows: one workgroup on a compute unit at most (it asks for as much as the unit can draw; 32 splits of 8 KV heads at 128K
+// tokens 57 us, 64 splits 73), and of those two blocks in each where there are many, since a split costs its merge 0.08 us (4095
+// tokens, 8 units, 8 / 16 / 32 splits 12.7 / 11.6 / 14.3 us; 2047 tokens 4 / 8 / 16 splits 12.1 / 10.4 / 11.1; one unit, 60000 tokens 32 /
+// 64 / 128 splits 24.9 / 21.7 / 24.4).  Up to four blocks are a wave's each in one workgroup, which spares the merge.
 int kv8_splits(const bd_paged8_cache* c, int max_tokens, int max_len) {
   const long rows = (long)max_tokens * (c->n_q_heads / c->n_kv_heads);
-  const bool few = kv8_few(rows);
-  const long units = (long)c->batch * c->n_kv_heads * (few ? (rows + 15) / 16 : (rows + 127) / 128);
-  const long blocks = (std::max(max_len, 1) - 1L) / kBlock + 1, quanta = few ? (blocks + 3) / 4 : (blocks + 7) / 8;
-  return (int)std::max(1L, std::min(quanta, 512 / std::max(1L, units)));
+  const long blocks = (std::max(max_len, 1) - 1L) / kBlock + 1;
+  if (kv8_few(rows)) {
+    const long units = (long)c->batch * c->n_kv_heads * ((rows + 15) / 16);
+    const long want = blocks <= 4 ? 1 : blocks <= 8 ? blocks : std::min(std::max(8L, blocks / 2), 64L);
+    return (int)std::max(1L, std::min(want, 256 / units));
+  }
+  const long units = (long)c->batch * c->n_kv_heads * ((rows + 127) / 128);
+  return (int)std::max(1L, std::min((blocks + 7) / 8, 512 / units));
 }
 
-hipError_t launch_kv8_attn(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, float* part,
+hipError_t launch_kv8_attn(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, void* ws,
                            void* out, hipStream_t st) {
-  const hipError_t e = (kv8_few((long)s.max_tokens * s.gq) ? launch_kv8_few : launch_kv8_many)(s, head_dim, code, elem, q, sc, splits, part, out, st);
+  if (kv8_few((long)s.max_tokens * s.gq)) return launch_kv8_few(s, head_dim, code, elem, q, sc, splits, ws, out, st);
+  float* part = (float*)((char*)ws + BD_PAGED8_COUNTER_BYTES);
+  const hipError_t e = launch_kv8_many(s, head_dim, code, elem, q, sc, splits, part, out, st);
   if (e != hipSuccess || splits == 1) return e;
   const dim3 grid((unsigned)(((long)s.max_tokens * s.n_q_heads + 3) / 4), s.batch);
 #define BD_RUN(D, E) hipLaunchKernelGGL((kv8_merge_kernel<D, E>), grid, dim3(256), 0, st, s, splits, part, (uint16_t*)out)
@@ -186,9 +196,14 @@ int32_t bd_paged8_choose_splits(const bd_paged8_cache* c, int32_t max_tokens, in
   return kv8_splits(c, max_tokens, max_len);
 }
 
-size_t bd_paged8_workspace_bytes(const bd_paged8_cache* c, int32_t total, int32_t num_splits) {
-  if (check_shape8(c) != BD_OK || total < 1 || num_splits < 2) return 0;
-  return (size_t)num_splits * total * c->n_q_heads * (c->head_dim + 2) * sizeof(float);
+size_t bd_paged8_workspace_bytes(const bd_paged8_cache* c, int32_t total, int32_t max_tokens, int32_t num_splits) {
+  if (check_shape8(c) != BD_OK || total < 1 || max_tokens < 1 || num_splits < 2) return 0;
+  const long gq = c->n_q_heads / c->n_kv_heads;
+  auto few = [&](long rows) { return (size_t)std::min(num_splits, kMostSplits) * c->batch * c->n_kv_heads * ((rows + 15) / 16) * std::min(rows, 16L); };
+  const long rows = std::min(max_tokens, total) * gq;
+  size_t filed = kv8_few(rows) ? few(rows) : (size_t)num_splits * total * c->n_q_heads;
+  if (kv8_few(gq)) filed = std::max(filed, few(gq));   // (a call without cu_tokens, whatever its max_tokens)
+  return BD_PAGED8_COUNTER_BYTES + filed * (c->head_dim + 2) * sizeof(float);
 }
 
 bd_status bd_paged8_attn(const bd_paged8_cache* c, const bd_rows* q, const int32_t* cu_tokens, int32_t total, int32_t max_tokens,
@@ -209,7 +224,7 @@ bd_status bd_paged8_attn(const bd_paged8_cache* c, const bd_rows* q, const int32
       ((long)st.max_tokens * c->n_q_heads + 3) / 4 > (1L << 24) - 1)
     return BD_ERR_UNSUPPORTED;
   const Scores8 sc{scores->softmax_scale, scores->softcap, scores->slopes, scores->prefix_lens, scores->window};
-  return hip_status(launch_kv8_attn(st, c->head_dim, c->code_type, c->elem_type, rows_of(q), sc, num_splits, (float*)workspace, out,
+  return hip_status(launch_kv8_attn(st, c->head_dim, c->code_type, c->elem_type, rows_of(q), sc, num_splits, workspace, out,
                                     (hipStream_t)stream));
 }
 

@@ -57,14 +57,22 @@ __device__ __forceinline__ h8_t query8(us8_t x, int shift) {
   return r;
 }
 
-// What a query row sees, and what is done to its scores.
-struct RowView {
-  int pos;      // index in the sequence
-  int prefix;   // of the sequence, at most its length
-  int window;   // 0: none
-  float slope;
-  __device__ __forceinline__ bool sees(int j) const { return j < prefix || (j <= pos && (window == 0 || pos - j < window)); }
+// step_rows for launches that write neither lengths nor lists, through the scalar cache
+struct ScalarLoad {
+  __device__ __forceinline__ int32_t operator()(const int32_t* p) const { return scalar_load(p); }
 };
+__device__ __forceinline__ bool queries_of(const Step8& s, int b, Seq8& q) { return step_rows(s, b, q, false, ScalarLoad()); }
+
+// What a query row sees, and what is done to its scores, by how far a token is before it (behind it: negative).  No token behind the
+// sequence's end is seen: rows and prefix end with it.
+struct RowView {
+  int pos;           // index in the sequence
+  int prefix;        // of the sequence, at most its length
+  uint32_t window;   // 2^31: none
+  float slope;
+};
+__device__ __forceinline__ uint32_t window_of(int window) { return window ? (uint32_t)window : 0x80000000u; }
+
 // natural units
 __device__ __forceinline__ float capped(float x, float cap, float inv_cap) {
   // tanh(y) = 1 - 2 / (1 + e^2y): within 2^-23 of it absolutely, which is what a score needs
@@ -95,18 +103,77 @@ __device__ __forceinline__ bool all_seen(int from, int lo, int hi, int prefix, i
   return from + kBlock <= prefix || (from + kBlock - 1 <= lo && (window == 0 || hi - from < window));
 }
 
+// N x 4 (or 16) scores of a row, as products, to natural units times log2 e, -infinity for tokens that the row does not see.  c: what a
+// product is worth; from + offset(t, i): the token.  Every pass is decided on once for all of them.
+template <class X, int N, class Offset>
+__device__ __forceinline__ void finish_scores(X* x, float c, const Scores8& sc, const RowView& view, bool masked, int from, Offset offset) {
+  constexpr int K = sizeof(X) / 4;
+  const int before = view.pos - from;
+  if (sc.cap > 0.f) {
+    const float inv_cap = 1.f / sc.cap;
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+      for (int i = 0; i < K; ++i) x[t][i] = capped(x[t][i] * c, sc.cap, inv_cap);
+    c = 1.f;
+  }
+  if (sc.slopes) {
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+      for (int i = 0; i < K; ++i) x[t][i] = x[t][i] * c - view.slope * (float)abs(before - offset(t, i));
+    c = 1.f;
+  }
+  c *= kLog2e;
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int i = 0; i < K; ++i) x[t][i] *= c;
+  if (masked) {
+    if (view.prefix > from) {
+      const int prefix = view.pos - view.prefix;
+#pragma unroll
+      for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+          const int y = before - offset(t, i);
+          if (y <= prefix && (uint32_t)y >= view.window) x[t][i] = -INFINITY;
+        }
+    } else {
+#pragma unroll
+      for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+          if ((uint32_t)(before - offset(t, i)) >= view.window) x[t][i] = -INFINITY;
+    }
+  }
+}
+template <class X, int N>
+__device__ __forceinline__ void no_scores(X* x) {
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(X) / 4); ++i) x[t][i] = -INFINITY;
+}
+
+// A page's number, -1 where the table has none, through the scalar cache: nothing of the launch writes the table, and a load that the
+// wave's vector loads need not be waited for with.
+__device__ __forceinline__ int page_in(const Step8& s, const int32_t* table, const Blocks& bl, int i) {
+  const int page = i < bl.count ? scalar_load(table + bl[i]) : -1;
+  return page < s.num_pages ? page : -1;   // (negative as it is)
+}
+__device__ __forceinline__ float scalar_scale(const float* p) { return __int_as_float(scalar_load((const int32_t*)p)); }
+
 // Logarithm (base 2) of the scale that the row sums are kept in units of: that of the first of the visible blocks (of up to 64)
 // with a scale.  A weight enters the product with V's codes times its block's scale, as an addend of its exponent, and the row sum
 // times 2^(reference - own): blocks whose values differ in size cost nothing, and a block of zeros counts as any other.
-__device__ __forceinline__ float scale_reference(const Step8& s, const Blocks& bl, int b, int h, int lane) {
-  float v = 0.f;
-  if (lane < bl.count) {
-    const int page = page_of(s, b, bl[lane]);
-    if (page >= 0) v = s.v_scales[(size_t)page * s.n_kv_heads + h];
+__device__ __forceinline__ float scale_reference(const Step8& s, const int32_t* table, const Blocks& bl, int h) {
+  for (int i = 0; i < min(bl.count, 64); ++i) {
+    const int page = page_in(s, table, bl, i);
+    const float v = page >= 0 ? scalar_scale(s.v_scales + (size_t)page * s.n_kv_heads + h) : 0.f;
+    if (v > 0.f) return log2f(v);
   }
-  const uint64_t some = __ballot(v > 0.f);
-  if (some == 0) return 0.f;
-  return log2f(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), __builtin_ctzll(some))));
+  return 0.f;
 }
 
 template <int ELEM>

@@ -9,7 +9,7 @@ namespace {
 // Per block  S^T = K Q^T  and  O^T += V^T P^T  with 16 x 16 x 32 products, tokens x rows and channels x rows: a lane holds
 // scores and outputs of one row, and its scores are, as they come, the eight tokens that the second product wants of the lane.
 // The order of tokens inside of the products is free, and chosen so that a lane's codes are 16 adjacent bytes: S^T's row 4 a + i of
-// tile t is token 32 a + 4 t + i, so lane group g has tokens 32 g .. 32 g + 31; likewise the channels of K.
+// tile t is token 64 (t / 4) + 16 a + 4 (t % 4) + i, so lane group g has tokens 16 g .. 16 g + 15 of each half; likewise the channels of K.
 template <int D, int CODE, int ELEM>
 struct Few {
   static constexpr int kChunks = D / 64, kSteps = D / 32, kTiles = D / 16;
@@ -20,25 +20,6 @@ struct Few {
   float m, l;    // running maximum (base 2, scale included) and sum of the lane's row
   f4_t acc[kTiles];
 
-  __device__ __forceinline__ void scores(f4_t* s, int n, float ck, int from, int stride, int per_tile, bool masked, int end, const Scores8& sc) const {
-    // s[t][i] is token from + stride * grp + per_tile * t + i
-    const bool plain = !(sc.cap > 0.f) && !sc.slopes;
-    const float inv_cap = sc.cap > 0.f ? 1.f / sc.cap : 0.f;
-#pragma unroll
-    for (int t = 0; t < n; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int j = from + stride * grp + per_tile * t + i;
-        float x = s[t][i] * (plain ? ck * kLog2e : ck);
-        if (!plain) {
-          if (sc.cap > 0.f) x = capped(x, sc.cap, inv_cap);
-          if (sc.slopes) x -= view.slope * (float)abs(view.pos - j);
-          x *= kLog2e;
-        }
-        if (masked && !(j < end && view.sees(j))) x = -INFINITY;
-        s[t][i] = x;
-      }
-  }
   // weights in place of scores; lv: the block's V scale, ref: the reference scale, both as logarithms
   __device__ __forceinline__ void weights(f4_t* s, int n, float lv, float ref) {
     float top = s[0][0];
@@ -66,16 +47,35 @@ struct Few {
   }
 };
 
+// Two floats past the L2 cache, to and from other XCDs' workgroups.
+__device__ __forceinline__ void put2(float* p, float a, float b) {
+  __hip_atomic_store((unsigned long long*)p, (unsigned long long)__float_as_uint(b) << 32 | __float_as_uint(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void get2(const float* p, float& a, float& b) {
+  const unsigned long long x = __hip_atomic_load((const unsigned long long*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  a = __uint_as_float((uint32_t)x);
+  b = __uint_as_float((uint32_t)(x >> 32));
+}
+
+// The weight of a partial result, given the largest maximum.
+__device__ __forceinline__ float merge_weight(float m, float top) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top); }
+
 template <int D, int CODE, int ELEM>
-__global__ __launch_bounds__(256, 2) void kv8_few_kernel(Step8 s, Rows8 q, Scores8 sc, int splits, float* part, uint16_t* out) {
+__global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Scores8 sc, int splits, Parts8 parts, uint16_t* out) {
   typedef Few<D, CODE, ELEM> F;
-  __shared__ float lds[4 * 16 * (D + 4) + 4 * 16 * 2];
+  constexpr int kPitch = D + 4;
+  __shared__ float lds[4 * 16 * kPitch + 4 * 16 * 2];
   const int b = blockIdx.z, h = blockIdx.y % s.n_kv_heads, tile = blockIdx.y / s.n_kv_heads, split = blockIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // (requested with the length, for where the wave's first block turns out to be the one of that number)
+  const int32_t* table = s.block_table + (size_t)b * s.max_pages;
+  const int guessed = split + splits * wave;
+  const int guess = guessed < s.max_pages ? scalar_load(table + guessed) : -1;
   Seq8 sq;
-  if (!step_rows(s, b, sq)) return;
+  if (!queries_of(s, b, sq)) return;
   const int rows = sq.n * s.gq;
   if (16 * tile >= rows) return;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int here = min(16, rows - 16 * tile);   // of the tile
   F f;
   f.lane = threadIdx.x & 63;
   f.col = f.lane & 15;
@@ -83,82 +83,126 @@ __global__ __launch_bounds__(256, 2) void kv8_few_kernel(Step8 s, Rows8 q, Score
   const int row = min(16 * tile + f.col, rows - 1), token = row / s.gq, head = h * s.gq + row % s.gq;
   const int length = sq.len + sq.n, lo = sq.len + 16 * tile / s.gq, hi = sq.len + min(16 * tile + 15, rows - 1) / s.gq;
   f.view.pos = sq.len + token;
-  f.view.prefix = sc.prefix ? min(max(sc.prefix[b], 0), length) : 0;
-  f.view.window = sc.window;
+  f.view.prefix = sc.prefix ? min(max(scalar_load(sc.prefix + b), 0), length) : 0;
+  f.view.window = window_of(sc.window);
   f.view.slope = sc.slopes ? sc.slopes[head] : 0.f;
   const uint16_t* q_row = q.data + (sq.row + token) * q.token + head * q.head;
   us8_t raw[F::kSteps];
-  uint32_t most = 0;
 #pragma unroll
-  for (int k = 0; k < F::kSteps; ++k) {
-    raw[k] = *(const us8_t*)(q_row + 64 * (k / 2) + 16 * f.grp + 8 * (k % 2));
-    most = max(most, most_of(raw[k]));
-  }
-  int shift = 0;
-  if (ELEM == BD_ELEM_BF16) {
-    most = __float_as_uint(join_groups(__uint_as_float(most), Max()));   // (bit patterns of positive numbers)
-    shift = bf16_shift(most);
-  }
+  for (int k = 0; k < F::kSteps; ++k) raw[k] = *(const us8_t*)(q_row + 64 * (k / 2) + 16 * f.grp + 8 * (k % 2));
+
+  // Blocks are dealt to the splits in turn, and a split's to its waves: a few blocks are one to a workgroup, on compute units of their own, since
+  // one of those draws some 35 GB/s whatever it asks for.  The residual goes, 32 tokens a wave, where the next block would.  No more splits
+  // than that are at work.
+  const Blocks blocks(lo, hi, length, f.view.prefix, sc.window, s.max_pages);
+  const int active = max(1, min(splits, blocks.count + blocks.tail));
+  if (split >= active) return;
+  const int begin = split + active * wave;
+  bool missing = blocks.lacks;
+  // (a block that is not there: any page's bytes, and none of its tokens seen)
+  u4_t kw[8][F::kChunks], vw[F::kTiles][2];
+  float ks, vs;
+  const size_t lane_k = (16 * (f.col >> 2) + (f.col & 3)) * D + 16 * f.grp, lane_v = f.col * kBlock + 16 * f.grp;
+  auto request_k = [&](int page) {
+    const size_t unit = (size_t)max(page, 0) * s.n_kv_heads + h;
+    const uint8_t* kc = s.k_codes + unit * (kBlock * D) + lane_k;
 #pragma unroll
-  for (int k = 0; k < F::kSteps; ++k) f.q[k] = query8<ELEM>(raw[k], shift);
-  f.c = ldexpf(sc.scale, -shift);
+    for (int t = 0; t < 8; ++t)
+#pragma unroll
+      for (int p = 0; p < F::kChunks; ++p) kw[t][p] = *(const u4_t*)(kc + (64 * (t / 4) + 4 * (t % 4)) * D + 64 * p);
+    ks = scalar_scale(s.k_scales + unit);
+  };
+  auto request_v = [&](int page) {
+    const size_t unit = (size_t)max(page, 0) * s.n_kv_heads + h;
+    const uint8_t* vc = s.v_codes + unit * (kBlock * D) + lane_v;
+#pragma unroll
+    for (int dt = 0; dt < F::kTiles; ++dt)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) vw[dt][u] = *(const u4_t*)(vc + 16 * dt * kBlock + 64 * u);
+    vs = scalar_scale(s.v_scales + unit);
+  };
   f.m = -INFINITY;
   f.l = 0.f;
 #pragma unroll
   for (int dt = 0; dt < F::kTiles; ++dt) f.acc[dt] = f4_t{0.f, 0.f, 0.f, 0.f};
-
-  const Blocks blocks(lo, hi, length, f.view.prefix, sc.window, s.max_pages);
-  const float ref = scale_reference(s, blocks, b, h, f.lane);
-  bool missing = blocks.lacks;
-  for (int it = 4 * split + wave; it < blocks.count; it += 4 * splits) {
-    const int block = blocks[it], page = __builtin_amdgcn_readfirstlane(page_of(s, b, block));
-    if (page < 0) {
-      missing = true;
-      continue;
+  float ref;
+  auto prepare = [&]() {   // (behind the first requests)
+    ref = scale_reference(s, table, blocks, h);
+    int shift = 0;
+    if (ELEM == BD_ELEM_BF16) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int k = 0; k < F::kSteps; ++k) most = max(most, most_of(raw[k]));
+      shift = bf16_shift(__float_as_uint(join_groups(__uint_as_float(most), Max())));   // (bit patterns of positive numbers)
     }
-    const size_t unit = (size_t)page * s.n_kv_heads + h;
-    const uint8_t* kc = s.k_codes + unit * (kBlock * D) + (32 * (f.col >> 2) + (f.col & 3)) * D + 16 * f.grp;
-    const uint8_t* vc = s.v_codes + unit * (kBlock * D) + f.col * kBlock + 32 * f.grp;
-    u4_t kw[8][F::kChunks], vw[F::kTiles][2];
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
-#pragma unroll
-      for (int p = 0; p < F::kChunks; ++p) kw[t][p] = *(const u4_t*)(kc + 4 * t * D + 64 * p);
-#pragma unroll
-    for (int dt = 0; dt < F::kTiles; ++dt)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) vw[dt][u] = *(const u4_t*)(vc + 16 * dt * kBlock + 16 * u);
-    const float ks = s.k_scales[unit], vs = s.v_scales[unit];
+    for (int k = 0; k < F::kSteps; ++k) f.q[k] = query8<ELEM>(raw[k], shift);
+    f.c = ldexpf(sc.scale, -shift);
+  };
+  if (begin < blocks.count) {
+    int it = begin, page = blocks.pre == 0 && blocks.first == 0 && begin == guessed ? (guess < s.num_pages ? guess : -1) : page_in(s, table, blocks, begin);
+    request_k(page);
+    request_v(page);
+    int next_page = page_in(s, table, blocks, it + 4 * active);
+    prepare();
     f4_t x[8];
+    int from;
+    float ck, lv;
+    bool gone;
+    auto products = [&]() {
+      from = blocks[it] * kBlock;
+      gone = page < 0;
+      missing |= gone;
+      ck = f.c * ks;
+      lv = vs > 0.f ? log2f(vs) : ref;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      x[t] = f4_t{0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < 8; ++t) {
+        x[t] = f4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int p = 0; p < F::kChunks; ++p) {
-        x[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<CODE>(kw[t][p][0], kw[t][p][1]), f.q[2 * p], x[t], 0, 0, 0);
-        x[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<CODE>(kw[t][p][2], kw[t][p][3]), f.q[2 * p + 1], x[t], 0, 0, 0);
+        for (int p = 0; p < F::kChunks; ++p) {
+          x[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<CODE>(kw[t][p][0], kw[t][p][1]), f.q[2 * p], x[t], 0, 0, 0);
+          x[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<CODE>(kw[t][p][2], kw[t][p][3]), f.q[2 * p + 1], x[t], 0, 0, 0);
+        }
       }
+    };
+    auto outputs = [&]() {
+      finish_scores<f4_t, 8>(x, ck, sc, f.view, !all_seen(from, lo, hi, f.view.prefix, sc.window), from + 16 * f.grp,
+                             [](int t, int i) { return 64 * (t / 4) + 4 * (t % 4) + i; });
+      if (gone) no_scores<f4_t, 8>(x);
+      f.weights(x, 8, lv, ref);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        h8_t p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = (_Float16)x[2 * k + e / 4][e % 4];
+#pragma unroll
+        for (int dt = 0; dt < F::kTiles; ++dt)
+          f.acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<CODE>(vw[dt][k / 2][2 * (k % 2)], vw[dt][k / 2][2 * (k % 2) + 1]), p, f.acc[dt], 0, 0, 0);
+      }
+    };
+    // The next block's keys are on their way while the scores and values are dealt with, its values behind them.  (The last block is
+    // written out once more: with the requests under a condition in the loop, the compiler waits for a block's values before its first product.)
+    products();
+    while (it + 4 * active < blocks.count) {
+      page = next_page;
+      request_k(page);
+      outputs();
+      request_v(page);
+      it += 4 * active;
+      next_page = page_in(s, table, blocks, it + 4 * active);
+      products();
     }
-    f.scores(x, 8, f.c * ks, block * kBlock, 32, 4, !all_seen(block * kBlock, lo, hi, f.view.prefix, sc.window), 0x7fffffff, sc);
-    f.weights(x, 8, vs > 0.f ? log2f(vs) : ref, ref);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      h8_t p;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = (_Float16)x[2 * k + e / 4][e % 4];
-#pragma unroll
-      for (int dt = 0; dt < F::kTiles; ++dt)
-        f.acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<CODE>(vw[dt][k / 2][2 * (k % 2)], vw[dt][k / 2][2 * (k % 2) + 1]), p, f.acc[dt], 0, 0, 0);
-    }
+    outputs();
+  } else {
+    prepare();
   }
   if (missing && s.status && f.lane == 0) atomicOr(s.status, kStatusRead);
 
-  // the residual: 32 tokens a wave, of the workgroup whose waves would be next
-  const int tail = length % kBlock, from = 32 * wave;
-  if (blocks.tail && split == (blocks.count + 3) / 4 % splits && from < tail) {
+  const int tail = length % kBlock, first = 32 * wave;
+  if (blocks.tail && split == blocks.count % active && first < tail) {
     const size_t unit = (size_t)b * s.n_kv_heads + h;
-    const uint16_t* kr = s.k_res + unit * (kBlock * D) + (from + 8 * (f.col >> 2) + (f.col & 3)) * D + 16 * f.grp;
-    const uint16_t* vr = s.v_res + unit * (kBlock * D) + (from + 8 * f.grp) * D + f.col;
+    const uint16_t* kr = s.k_res + unit * (kBlock * D) + (first + 8 * (f.col >> 2) + (f.col & 3)) * D + 16 * f.grp;
+    const uint16_t* vr = s.v_res + unit * (kBlock * D) + (first + 8 * f.grp) * D + f.col;
     us8_t kx[2][F::kSteps], vx[F::kTiles];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -167,7 +211,7 @@ __global__ __launch_bounds__(256, 2) void kv8_few_kernel(Step8 s, Rows8 q, Score
 #pragma unroll
     for (int dt = 0; dt < F::kTiles; ++dt)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) vx[dt][e] = from + 8 * f.grp + e < tail ? vr[e * D + 16 * dt] : (uint16_t)0;   // (rows behind the last are anything)
+      for (int e = 0; e < 8; ++e) vx[dt][e] = first + 8 * f.grp + e < tail ? vr[e * D + 16 * dt] : (uint16_t)0;   // (rows behind the last are anything)
     f4_t x[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -177,10 +221,10 @@ __global__ __launch_bounds__(256, 2) void kv8_few_kernel(Step8 s, Rows8 q, Score
         if (ELEM == BD_ELEM_F16)
           x[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, kx[t][k]), f.q[k], x[t], 0, 0, 0);
         else
-          x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8_t, kx[t][k]), __builtin_bit_cast(bf8_t, raw[k]), x[t], 0, 0, 0);
+          x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8_t, kx[t][k]), *(const bf8_t*)(q_row + 64 * (k / 2) + 16 * f.grp + 8 * (k % 2)), x[t], 0, 0, 0);
       }
     }
-    f.scores(x, 2, sc.scale, length - tail + from, 8, 4, true, length, sc);
+    finish_scores<f4_t, 2>(x, sc.scale, sc, f.view, true, length - tail + first + 8 * f.grp, [](int t, int i) { return 4 * t + i; });
     f.weights(x, 2, 0.f, ref);
     if (ELEM == BD_ELEM_F16) {
       h8_t p;
@@ -206,47 +250,148 @@ __global__ __launch_bounds__(256, 2) void kv8_few_kernel(Step8 s, Rows8 q, Score
   }
 
   // the four waves' results, in units of 2^(m - kShift) and, the sums, of 2^ref
-  float* ml = lds + 4 * 16 * (D + 4);
-  if (f.grp == 0) {
-    ml[(wave * 16 + f.col) * 2] = f.m;
-    ml[(wave * 16 + f.col) * 2 + 1] = f.l;
-  }
+  float* ml = lds + 4 * 16 * kPitch;
+  if (f.col < here) {
+    if (f.grp == 0) {
+      ml[(wave * 16 + f.col) * 2] = f.m;
+      ml[(wave * 16 + f.col) * 2 + 1] = f.l;
+    }
 #pragma unroll
-  for (int dt = 0; dt < F::kTiles; ++dt) *(f4_t*)(lds + (wave * 16 + f.col) * (D + 4) + 16 * dt + 4 * f.grp) = f.acc[dt];
+    for (int dt = 0; dt < F::kTiles; ++dt) *(f4_t*)(lds + (wave * 16 + f.col) * kPitch + 16 * dt + 4 * f.grp) = f.acc[dt];
+  }
   __syncthreads();
   constexpr int kPer = D / 16;   // channels a thread
   const int r = threadIdx.x / 16, d = threadIdx.x % 16 * kPer;
-  if (16 * tile + r >= rows) return;
-  float top = -INFINITY;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[(w * 16 + r) * 2]);
-  float o[kPer] = {}, sum = 0.f;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float fac = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[(w * 16 + r) * 2] - top);
-    sum += fac * ml[(w * 16 + r) * 2 + 1];
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) o[e] += fac * lds[(w * 16 + r) * (D + 4) + d + e];
-  }
   const float unit = __builtin_amdgcn_exp2f(ref);
-  const int tk = (16 * tile + r) / s.gq, hd = h * s.gq + (16 * tile + r) % s.gq;
-  const size_t at = (size_t)(sq.row + tk) * s.n_q_heads + hd;
-  if (splits > 1) {
-    store_part<D, kPer>(part, splits, (size_t)s.total * s.n_q_heads, split, at, d, o, unit, top, sum);
+  float o[kPer] = {}, sum = 0.f, top = -INFINITY;
+  if (r < here) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[(w * 16 + r) * 2]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float fac = merge_weight(ml[(w * 16 + r) * 2], top);
+      sum += fac * ml[(w * 16 + r) * 2 + 1];
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) o[e] += fac * lds[(w * 16 + r) * kPitch + d + e];
+    }
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) o[e] *= unit;
+  }
+  const size_t token_row = sq.row * (size_t)s.n_q_heads;
+  auto out_row = [&](int i) { return token_row + (size_t)((16 * tile + i) / s.gq) * s.n_q_heads + h * s.gq + (16 * tile + i) % s.gq; };
+  if (active == 1) {
+    if (r >= here) return;
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int e = 0; e < kPer; e += 2) *(uint32_t*)(out + out_row(r) * D + d + e) = elem2<ELEM>(o[e] * inv, o[e + 1] * inv);
     return;
   }
-  const float inv = sum > 0.f ? unit / sum : 0.f;
+
+  // The workgroup that files the last of the partial results merges them, which spares a launch.  They pass between XCDs, whose L2
+  // caches do not know of each other: device-scope stores and loads, which go through those, so that no cache has to be written back or emptied
+  // (as a release and an acquire at that scope would); a store is waited for before it is counted.
+  const int units = s.batch * (int)gridDim.y, at = b * (int)gridDim.y + blockIdx.y;
+  const int filed = min(16, s.max_tokens * s.gq);   // rows of a partial result
+  float* po = parts.data + (size_t)at * splits * filed * D;
+  float* pml = parts.data + (size_t)units * splits * filed * D + (size_t)at * splits * filed * 2;
+  if (r < here) {
 #pragma unroll
-  for (int e = 0; e < kPer; e += 2) *(uint32_t*)(out + at * D + d + e) = elem2<ELEM>(o[e] * inv, o[e + 1] * inv);
+    for (int e = 0; e < kPer; e += 2) put2(po + (split * filed + r) * D + d + e, o[e], o[e + 1]);
+    if (d == 0) put2(pml + (split * filed + r) * 2, top, sum);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  uint32_t* seen = (uint32_t*)lds;
+  if (threadIdx.x == 0) {
+    const uint32_t n = __hip_atomic_fetch_add(parts.counters + at, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
+    if (n == (uint32_t)active) __hip_atomic_store(parts.counters + at, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *seen = n;
+  }
+  __syncthreads();
+  if (*seen != (uint32_t)active) return;
+  __syncthreads();
+  // outputs: rows x slices of the splits fill the workgroup; a thread's first ones are on their way with the maxima and sums
+  const int held = here > 8 ? 16 : here > 4 ? 8 : here > 2 ? 4 : here, slices = 16 / held, mr = r % held, slice = r / held;
+  constexpr int kAhead = 8;
+  float ahead[kAhead][kPer];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+    for (int e = 0; e < kPer; e += 2) {
+      ahead[i][e] = ahead[i][e + 1] = 0.f;
+      if (slice + i * slices < active && mr < here) get2(po + ((slice + i * slices) * filed + mr) * D + d + e, ahead[i][e], ahead[i][e + 1]);
+    }
+  // a row's maxima and sums by 16 threads
+  float* fac = lds;                            // [16][kMostSplits] weights of the partial results
+  float* sums = lds + 16 * kMostSplits;        // [16]
+  float* slices_o = sums + 16;                 // [slice][row][D]
+  const int lane16 = threadIdx.x % 16;
+  float all = -INFINITY, mm[kMostSplits / 16], ll[kMostSplits / 16];
+#pragma unroll
+  for (int i = 0; i < kMostSplits / 16; ++i) {
+    mm[i] = -INFINITY;
+    ll[i] = 0.f;
+    if (16 * i + lane16 < active && r < here) get2(pml + ((16 * i + lane16) * filed + r) * 2, mm[i], ll[i]);
+    all = fmaxf(all, mm[i]);
+  }
+#pragma unroll
+  for (int x = 1; x < 16; x *= 2) all = fmaxf(all, __shfl_xor(all, x));
+  float l = 0.f;
+#pragma unroll
+  for (int i = 0; i < kMostSplits / 16; ++i) {
+    const float w = merge_weight(mm[i], all);
+    l += w * ll[i];
+    fac[r * kMostSplits + 16 * i + lane16] = w;
+  }
+#pragma unroll
+  for (int x = 1; x < 16; x *= 2) l += __shfl_xor(l, x);
+  if (lane16 == 0) sums[r] = l;
+  __syncthreads();
+  float acc[kPer] = {};
+  if (mr < here) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (slice + i * slices >= active) break;
+      const float w = fac[mr * kMostSplits + slice + i * slices];
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) acc[e] += w * ahead[i][e];
+    }
+#pragma unroll 8
+    for (int k = slice + kAhead * slices; k < active; k += slices) {
+      const float w = fac[mr * kMostSplits + k];
+#pragma unroll
+      for (int e = 0; e < kPer; e += 2) {
+        float y0, y1;
+        get2(po + (k * filed + mr) * D + d + e, y0, y1);
+        acc[e] += w * y0;
+        acc[e + 1] += w * y1;
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < kPer; e += 4) *(f4_t*)(slices_o + r * kPitch + d + e) = f4_t{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+  __syncthreads();
+  if (r >= here) return;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) o[e] = 0.f;
+  for (int k = 0; k < slices; ++k)
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) o[e] += slices_o[(k * held + r) * kPitch + d + e];
+  const float inv = sums[r] > 0.f ? 1.f / sums[r] : 0.f;
+#pragma unroll
+  for (int e = 0; e < kPer; e += 2) *(uint32_t*)(out + out_row(r) * D + d + e) = elem2<ELEM>(o[e] * inv, o[e + 1] * inv);
 }
 
 }  // namespace
 
-hipError_t launch_kv8_few(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, float* part,
-                          void* out, hipStream_t st) {
-  const int tiles = (int)(((long)s.max_tokens * s.gq + 15) / 16);
-  const dim3 grid(splits, s.n_kv_heads * tiles, s.batch);
-#define BD_RUN(D, C, E) hipLaunchKernelGGL((kv8_few_kernel<D, C, E>), grid, dim3(256), 0, st, s, q, sc, splits, part, (uint16_t*)out)
+hipError_t launch_kv8_few(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, void* ws, void* out,
+                          hipStream_t st) {
+  const long tiles = ((long)s.max_tokens * s.gq + 15) / 16;
+  if (s.n_kv_heads * tiles * s.batch > kCounters) splits = 1;   // (far more workgroups than the chip holds)
+  splits = splits < kMostSplits ? splits : kMostSplits;
+  const Parts8 parts{(uint32_t*)ws, (float*)((char*)ws + BD_PAGED8_COUNTER_BYTES)};
+  const dim3 grid(splits, (unsigned)(s.n_kv_heads * tiles), s.batch);
+#define BD_RUN(D, C, E) hipLaunchKernelGGL((kv8_few_kernel<D, C, E>), grid, dim3(256), 0, st, s, q, sc, splits, parts, (uint16_t*)out)
   BD_KV8_INSTANCES(head_dim, code, elem, BD_RUN)
 #undef BD_RUN
   return hipGetLastError();

@@ -19,7 +19,7 @@ __global__ __launch_bounds__(256, 2) void kv8_many_kernel(Step8 s, Rows8 q, Scor
   const int h = blockIdx.x, b = blockIdx.z;
   const int tile = (int)(gridDim.y / splits - 1 - blockIdx.y / splits), split = blockIdx.y % splits;   // (the longest first)
   Seq8 sq;
-  if (!step_rows(s, b, sq)) return;
+  if (!queries_of(s, b, sq)) return;
   const int rows = sq.n * s.gq;
   if (kManyRows * tile >= rows) return;
   const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
@@ -31,11 +31,9 @@ __global__ __launch_bounds__(256, 2) void kv8_many_kernel(Step8 s, Rows8 q, Scor
   const int wave_lo = sq.len + min(first_row, rows - 1) / s.gq, wave_hi = sq.len + min(first_row + 31, rows - 1) / s.gq;
   RowView view;
   view.pos = sq.len + token;
-  view.prefix = sc.prefix ? min(max(sc.prefix[b], 0), length) : 0;
-  view.window = sc.window;
+  view.prefix = sc.prefix ? min(max(scalar_load(sc.prefix + b), 0), length) : 0;
+  view.window = window_of(sc.window);
   view.slope = sc.slopes ? sc.slopes[head] : 0.f;
-  const bool plain = !(sc.cap > 0.f) && !sc.slopes;
-  const float inv_cap = sc.cap > 0.f ? 1.f / sc.cap : 0.f;
 
   const uint16_t* q_row = q.data + (sq.row + token) * q.token + head * q.head + 8 * half;
   h8_t qf[kSteps];
@@ -55,7 +53,8 @@ __global__ __launch_bounds__(256, 2) void kv8_many_kernel(Step8 s, Rows8 q, Scor
   const float c = ldexpf(sc.scale, -shift);
 
   const Blocks blocks(lo, hi, length, view.prefix, sc.window, s.max_pages);
-  const float ref = scale_reference(s, blocks, b, h, lane);
+  const int32_t* table = s.block_table + (size_t)b * s.max_pages;
+  const float ref = scale_reference(s, table, blocks, h);
   float m = -INFINITY, l = 0.f;
   f16x_t acc[kTiles];
 #pragma unroll
@@ -74,24 +73,14 @@ __global__ __launch_bounds__(256, 2) void kv8_many_kernel(Step8 s, Rows8 q, Scor
   };
   // scores to weights; returns nothing, changes m, l, acc
   f16x_t x[4];
-  auto weigh = [&](int from, float ck, bool masked, int end, float lv) {
-    const float ck2 = plain ? ck * kLog2e : ck;
+  auto weigh = [&](int from, float ck, bool masked, bool gone, float lv) {
+    finish_scores<f16x_t, 4>(x, ck, sc, view, masked, from + 8 * half, [](int t, int i) { return 32 * t + 16 * (i / 8) + i % 8; });
+    if (gone) no_scores<f16x_t, 4>(x);
     float top = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float y = x[t][i] * ck2;
-        const int j = from + 32 * t + 16 * (i / 8) + 8 * half + i % 8;
-        if (!plain) {
-          if (sc.cap > 0.f) y = capped(y, sc.cap, inv_cap);
-          if (sc.slopes) y -= view.slope * (float)abs(view.pos - j);
-          y *= kLog2e;
-        }
-        if (masked && !(j < end && view.sees(j))) y = -INFINITY;
-        x[t][i] = y;
-        top = fmaxf(top, y);
-      }
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, x[t][i]);
     top = join_xor32(top, Max()) + lv;
     const float now = fmaxf(m, top), base = now == -INFINITY ? 0.f : now;
     const float was = __builtin_amdgcn_exp2f(m - base), off = lv - base + kShift;
@@ -116,17 +105,9 @@ __global__ __launch_bounds__(256, 2) void kv8_many_kernel(Step8 s, Rows8 q, Scor
   // this split's blocks, the residual with the last split
   const int begin = (int)((long)blocks.count * split / splits), end = (int)((long)blocks.count * (split + 1) / splits);
   u4_t kw[kUnits], vw[kUnits];
-  int page = -1, next = begin;
   bool missing = blocks.lacks;
-  auto request = [&](int it) {   // the next block that is there, from `it` on
-    page = -1;
-    for (next = it; next < end; ++next) {
-      page = __builtin_amdgcn_readfirstlane(page_of(s, b, blocks[next]));
-      if (page >= 0) break;
-      missing = true;
-    }
-    if (page < 0) return;
-    const size_t unit = (size_t)page * s.n_kv_heads + h;
+  auto request = [&](int page) {   // (a block that is not there: any page's bytes, and none of its tokens seen)
+    const size_t unit = (size_t)max(page, 0) * s.n_kv_heads + h;
     const u4_t* kc = (const u4_t*)(s.k_codes + unit * (kBlock * D));
     const u4_t* vc = (const u4_t*)(s.v_codes + unit * (kBlock * D));
 #pragma unroll
@@ -135,11 +116,15 @@ __global__ __launch_bounds__(256, 2) void kv8_many_kernel(Step8 s, Rows8 q, Scor
       vw[n] = vc[n * 256 + threadIdx.x];
     }
   };
-  request(begin);
-  while (page >= 0) {
-    const int block = blocks[next];
-    const size_t unit = (size_t)page * s.n_kv_heads + h;
-    const float ks = s.k_scales[unit], vs = s.v_scales[unit];
+  int next_page = page_in(s, table, blocks, begin);
+  if (begin < end) request(next_page);
+  for (int it = begin; it < end; ++it) {
+    const int page = next_page, from = blocks[it] * kBlock;
+    const bool gone = page < 0;
+    missing |= gone;
+    next_page = page_in(s, table, blocks, it + 1);
+    const size_t unit = (size_t)max(page, 0) * s.n_kv_heads + h;
+    const float ks = scalar_scale(s.k_scales + unit), vs = scalar_scale(s.v_scales + unit);
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < kUnits; ++n) {
@@ -151,7 +136,7 @@ __global__ __launch_bounds__(256, 2) void kv8_many_kernel(Step8 s, Rows8 q, Scor
       *(h8_t*)(lds_v + vr * kBlock + 8 * ((vx + 1) ^ (vr & 15))) = codes8<CODE>(vw[n][2], vw[n][3]);
     }
     __syncthreads();
-    request(next + 1);
+    if (it + 1 < end) request(next_page);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
 #pragma unroll
@@ -159,7 +144,7 @@ __global__ __launch_bounds__(256, 2) void kv8_many_kernel(Step8 s, Rows8 q, Scor
 #pragma unroll
       for (int k = 0; k < kSteps; ++k) x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(frag_k(t, k), qf[k], x[t], 0, 0, 0);
     }
-    weigh(block * kBlock, c * ks, !all_seen(block * kBlock, wave_lo, wave_hi, view.prefix, sc.window), 0x7fffffff, vs > 0.f ? log2f(vs) : ref);
+    weigh(from, c * ks, !all_seen(from, wave_lo, wave_hi, view.prefix, sc.window), gone, vs > 0.f ? log2f(vs) : ref);
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -207,7 +192,7 @@ __global__ __launch_bounds__(256, 2) void kv8_many_kernel(Step8 s, Rows8 q, Scor
           x[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8_t, frag_k(t, k)), *(const bf8_t*)(q_row + 16 * k), x[t], 0, 0, 0);
       }
     }
-    weigh(length - tail, sc.scale, true, length, 0.f);
+    weigh(length - tail, sc.scale, true, false, 0.f);
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll

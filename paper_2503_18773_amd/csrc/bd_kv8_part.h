@@ -5,8 +5,17 @@
 
 namespace bd {
 
-hipError_t launch_kv8_few(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, float* part,
-                          void* out, hipStream_t st);
+// Few rows: the launch merges its splits' partial results itself, in up to kMostSplits of them, with a counter for each of up to
+// kCounters units (sequence, KV head, tile of 16 rows).  Workspace: the counters, then [unit][split][rows][D] unnormalised outputs and [unit][split]
+// [rows][2] maxima (base 2) and sums.
+constexpr int kMostSplits = 128;
+constexpr long kCounters = BD_PAGED8_COUNTER_BYTES / 4;
+struct Parts8 {
+  uint32_t* counters;
+  float* data;
+};
+hipError_t launch_kv8_few(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, void* ws, void* out,
+                          hipStream_t st);
 hipError_t launch_kv8_many(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, float* part,
                            void* out, hipStream_t st);
 
@@ -25,7 +34,7 @@ hipError_t launch_kv8_many(const Step8& s, int head_dim, int code, int elem, con
 
 namespace {
 
-// Workspace: [splits][rows][D] unnormalised outputs, then [splits][rows][2] maxima (base 2) and sums; a row is (token, query head).
+// Many rows: behind the counters, [splits][rows][D] unnormalised outputs, then [splits][rows][2] maxima (base 2) and sums; a row is (token, query head).
 template <int D, int N>
 __device__ __forceinline__ void store_part(float* part, int splits, size_t rows, int split, size_t row, int d, const float* o, float unit,
                                            float m, float l) {

@@ -1,5 +1,6 @@
 """The paged 8-bit cache on the CPU: the oracle's pieces against other ways to say the same, and what the library refuses."""
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -93,8 +94,14 @@ def test_sizes_and_splits():
                 dict(max_pages_per_seq=-1), dict(batch=65536), dict(n_q_heads=32768)):
         assert B.bd_paged8_cache_bytes(_desc(**bad), 0) == 0
     assert B.bd_paged8_cache_bytes(c, -1) == 0
-    assert B.bd_paged8_workspace_bytes(c, 10, 1) == 0 and B.bd_paged8_workspace_bytes(c, 10, 3) == 3 * 10 * 8 * 130 * 4
-    assert B.bd_paged8_workspace_bytes(c, 0, 3) == 0
+    # counters, then a row and split each: of few rows padded to tiles of 16 rows, in up to 128 splits
+    size = lambda *a: B.bd_paged8_workspace_bytes(c, *a) - 65536   # noqa: E731
+    assert B.bd_paged8_workspace_bytes(c, 10, 4, 1) == B.bd_paged8_workspace_bytes(c, 0, 4, 3) == B.bd_paged8_workspace_bytes(c, 9, 0, 3) == 0
+    assert size(4, 1, 3) == size(4, 1, 3) == 3 * 4 * 2 * 4 * 130 * 4 and size(20, 5, 3) == 3 * 4 * 2 * 32 * 130 * 4
+    wide = _desc(n_q_heads=34)   # (17 a group: without cu_tokens the rows are few, whatever is said of max_tokens)
+    assert B.bd_paged8_workspace_bytes(wide, 4, 100, 3) - 65536 >= 3 * 4 * 2 * 32 * 130 * 4
+    assert size(4, 1, 128) == size(4, 1, 9999) == 128 * 32 * 130 * 4 and size(500, 200, 3) == 3 * 500 * 8 * 130 * 4
+    assert "#define BD_PAGED8_COUNTER_BYTES 65536\n" in open(os.path.join(os.path.dirname(B._LIB_PATH), "..", "include", "bitdecode.h")).read()
     for tokens in (1, 3, 17, 300, 5000):
         for length in (1, 128, 129, 5000, 1 << 20, 2 ** 31 - 1):
             assert 1 <= B.bd_paged8_choose_splits(c, tokens, length) <= (length + 127) // 128
@@ -151,16 +158,22 @@ def test_what_is_refused_before_anything_is_launched():
 
 
 @needs_lib
-def test_the_class_checks_its_tensors():
+@pytest.mark.parametrize("call", ["ctypes", "module"])
+def test_the_class_checks_its_tensors(call, monkeypatch):
+    """Both ways that the class calls the library (the C module may not have been built)."""
+    if call == "ctypes":
+        monkeypatch.setattr(B, "_call", B._CtypesCall)
+    stream = type("", (), {"cuda_stream": 0})
     c = B.PagedKV8Cache(2, 4, 2, "int8", 6, [[0, 1, 2], [3, 4, 5]], head_dim=64, device="cpu")   # (a description; nothing is launched)
     assert c.max_len == 4 * 128 - 1 and c.k_codes.numel() == 6 * 2 * 128 * 64
     k, q, out = (torch.zeros(2, h, 64, dtype=torch.float16) for h in (2, 4, 4))
-    for bad in (lambda: c.append(k.float(), k), lambda: c.append(k[:, :1], k), lambda: c.append(k, k[:1]), lambda: c.append(k, k, q=q),
-                lambda: c.append(k, k, q=q, q_out=out[:1]), lambda: c.append(k.transpose(0, 2).contiguous().transpose(0, 2), k),
-                lambda: c.append(k, k, cu_tokens=torch.zeros(2, dtype=torch.int32)), lambda: c.append(k, k, cu_tokens=torch.zeros(3, dtype=torch.int64)),
-                lambda: c.attn(q, 1.0, out[:1]), lambda: c.attn(q, 1.0, torch.zeros(2, 4, 128, dtype=torch.float16)[..., :64]),
-                lambda: c.attn(q, 1.0, out, slopes=torch.zeros(2)), lambda: c.attn(q, 1.0, out, prefix_lens=torch.zeros(2)),
-                lambda: c.append(k, k, rotation=B.Rotation(torch.zeros(9, 32), positions=torch.zeros(3, dtype=torch.int32))),
+    append, attn = functools.partial(c.append, stream=stream), functools.partial(c.attn, stream=stream)
+    for bad in (lambda: append(k.float(), k), lambda: append(k[:, :1], k), lambda: append(k, k[:1]), lambda: append(k, k, q=q),
+                lambda: append(k, k, q=q, q_out=out[:1]), lambda: append(k.transpose(0, 2).contiguous().transpose(0, 2), k),
+                lambda: append(k, k, cu_tokens=torch.zeros(2, dtype=torch.int32)), lambda: append(k, k, cu_tokens=torch.zeros(3, dtype=torch.int64)),
+                lambda: attn(q, 1.0, out[:1]), lambda: attn(q, 1.0, torch.zeros(2, 4, 128, dtype=torch.float16)[..., :64]),
+                lambda: attn(q, 1.0, out, slopes=torch.zeros(2)), lambda: attn(q, 1.0, out, prefix_lens=torch.zeros(2)),
+                lambda: append(k, k, rotation=B.Rotation(torch.zeros(9, 32), positions=torch.zeros(3, dtype=torch.int32))),
                 lambda: B.Rotation(torch.zeros(9, 32).double()), lambda: B.Rotation(torch.zeros(9, 32), positions=torch.zeros(3)),
                 lambda: B.PagedKV8Cache(2, 4, 2, "int4", 6, [[0], [1]], device="cpu"), lambda: B.PagedKV8Cache(2, 4, 2, "int8", 6, [[0]], device="cpu"),
                 lambda: B.PagedKV8Cache(2, 4, 2, "int8", 6, [[0], [1]], dtype=torch.float32, device="cpu"),
@@ -171,4 +184,4 @@ def test_the_class_checks_its_tensors():
     with pytest.raises(B.BitDecodeError):
         B.PagedKV8Cache(2, 4, 3, "int8", 6, [[0], [1]], device="cpu")
     with pytest.raises(B.BitDecodeError):
-        c.append(k, k, rotation=B.Rotation(torch.zeros(9, 24)), stream=type("", (), {"cuda_stream": 0}))
+        c.append(k, k, rotation=B.Rotation(torch.zeros(9, 24)), stream=stream)
