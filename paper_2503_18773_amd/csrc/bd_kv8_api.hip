@@ -124,8 +124,8 @@ int kv8_splits(const bd_paged8_cache* c, int max_tokens, int max_len) {
     const long want = blocks <= 4 ? 1 : blocks <= 8 ? blocks : std::min(std::max(8L, blocks / 2), 64L);
     return (int)std::max(1L, std::min(want, 256 / units));
   }
-  const long units = (long)c->batch * c->n_kv_heads * ((rows + 127) / 128);
-  return (int)std::max(1L, std::min((blocks + 7) / 8, 512 / units));
+  const long units = (long)c->batch * c->n_kv_heads * ((rows + many_rows(c->head_dim) - 1) / many_rows(c->head_dim));
+  return (int)std::max(1L, std::min((blocks + 7) / 8, 256 / units));
 }
 
 hipError_t launch_kv8_attn(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, void* ws,
@@ -220,7 +220,7 @@ bd_status bd_paged8_attn(const bd_paged8_cache* c, const bd_rows* q, const int32
   const Step8 st = step_of(c, cu_tokens, total, max_tokens);
   const long rows = (long)st.max_tokens * st.gq;
   // launch grid dimensions: KV heads x tiles of rows, tiles x splits; the merge's rows
-  if (num_splits > 65535 || (kv8_few(rows) ? (rows + 15) / 16 * c->n_kv_heads : (rows + 127) / 128 * num_splits) > 65535 ||
+  if (num_splits > 65535 || (kv8_few(rows) ? (rows + 15) / 16 * c->n_kv_heads : (rows + many_rows(c->head_dim) - 1) / many_rows(c->head_dim) * num_splits) > 65535 ||
       ((long)st.max_tokens * c->n_q_heads + 3) / 4 > (1L << 24) - 1)
     return BD_ERR_UNSUPPORTED;
   const Scores8 sc{scores->softmax_scale, scores->softcap, scores->slopes, scores->prefix_lens, scores->window};

@@ -73,13 +73,6 @@ struct RowView {
 };
 __device__ __forceinline__ uint32_t window_of(int window) { return window ? (uint32_t)window : 0x80000000u; }
 
-// natural units
-__device__ __forceinline__ float capped(float x, float cap, float inv_cap) {
-  // tanh(y) = 1 - 2 / (1 + e^2y): within 2^-23 of it absolutely, which is what a score needs
-  const float e = __builtin_amdgcn_exp2f(x * inv_cap * (2.f * kLog2e));
-  return cap - 2.f * cap * __builtin_amdgcn_rcpf(1.f + e);
-}
-
 // The blocks of a sequence that queries at positions lo .. hi can see: [0, pre) and [first, ...), `count` in all that the table has room
 // for; whether it lacks some; and whether they can see the residual behind the whole blocks.
 struct Blocks {
@@ -103,50 +96,49 @@ __device__ __forceinline__ bool all_seen(int from, int lo, int hi, int prefix, i
   return from + kBlock <= prefix || (from + kBlock - 1 <= lo && (window == 0 || hi - from < window));
 }
 
-// N x 4 (or 16) scores of a row, as products, to natural units times log2 e, -infinity for tokens that the row does not see.  c: what a
-// product is worth; from + offset(t, i): the token.  Every pass is decided on once for all of them.
+// A score in units of log2 e is x * by + plus, of what finish_scores leaves in x: its multiplication is one with what the exponential's
+// argument needs anyway, and the largest x is the largest score (by > 0).
+struct Linear {
+  float by, plus;
+};
+
+// N x 4 (or 16) products of a row to scores, -infinity for tokens that the row does not see.  c >= 0: what a product is worth, in natural
+// units; from + offset(t, i): the token.  Every pass is decided on once for all of them.
+// The cap: cap tanh(y) = cap + 2 cap r with r = -1 / (1 + e^2y), within 2^-23 of it absolutely, which is what a score needs.
 template <class X, int N, class Offset>
-__device__ __forceinline__ void finish_scores(X* x, float c, const Scores8& sc, const RowView& view, bool masked, int from, Offset offset) {
+__device__ __forceinline__ Linear finish_scores(X* x, float c, const Scores8& sc, const RowView& view, bool masked, int from, Offset offset) {
   constexpr int K = sizeof(X) / 4;
-  const int before = view.pos - from;
+  Linear f{fmaxf(c * kLog2e, 1e-30f), 0.f};   // (0 times -infinity is no score)
   if (sc.cap > 0.f) {
-    const float inv_cap = 1.f / sc.cap;
+    const float twice = 2.f * kLog2e * c / sc.cap;
 #pragma unroll
     for (int t = 0; t < N; ++t)
 #pragma unroll
-      for (int i = 0; i < K; ++i) x[t][i] = capped(x[t][i] * c, sc.cap, inv_cap);
-    c = 1.f;
+      for (int i = 0; i < K; ++i) x[t][i] = __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(x[t][i] * twice));
+    f = Linear{2.f * kLog2e * sc.cap, kLog2e * sc.cap};
   }
+  // (how far the tokens are before the row, in each pass for itself: for both the compiler would keep them all in registers)
+  int before = view.pos - from;
   if (sc.slopes) {
+    const float distance = (float)before, slope = view.slope * kLog2e;
 #pragma unroll
     for (int t = 0; t < N; ++t)
 #pragma unroll
-      for (int i = 0; i < K; ++i) x[t][i] = x[t][i] * c - view.slope * (float)abs(before - offset(t, i));
-    c = 1.f;
+      for (int i = 0; i < K; ++i) x[t][i] = fmaf(-slope, fabsf(distance - (float)offset(t, i)), fmaf(x[t][i], f.by, f.plus));
+    f = Linear{1.f, 0.f};
   }
-  c *= kLog2e;
-#pragma unroll
-  for (int t = 0; t < N; ++t)
-#pragma unroll
-    for (int i = 0; i < K; ++i) x[t][i] *= c;
+  asm volatile("" : "+v"(before));
   if (masked) {
-    if (view.prefix > from) {
-      const int prefix = view.pos - view.prefix;
+    const int prefix = view.pos - view.prefix;   // (how far a row is behind the prefix's end)
 #pragma unroll
-      for (int t = 0; t < N; ++t)
+    for (int t = 0; t < N; ++t)
 #pragma unroll
-        for (int i = 0; i < K; ++i) {
-          const int y = before - offset(t, i);
-          if (y <= prefix && (uint32_t)y >= view.window) x[t][i] = -INFINITY;
-        }
-    } else {
-#pragma unroll
-      for (int t = 0; t < N; ++t)
-#pragma unroll
-        for (int i = 0; i < K; ++i)
-          if ((uint32_t)(before - offset(t, i)) >= view.window) x[t][i] = -INFINITY;
-    }
+      for (int i = 0; i < K; ++i) {
+        const int y = before - offset(t, i);
+        x[t][i] = ((y <= prefix) & ((uint32_t)y >= view.window)) ? -INFINITY : x[t][i];
+      }
   }
+  return f;
 }
 template <class X, int N>
 __device__ __forceinline__ void no_scores(X* x) {

@@ -21,21 +21,21 @@ struct Few {
   f4_t acc[kTiles];
 
   // weights in place of scores; lv: the block's V scale, ref: the reference scale, both as logarithms
-  __device__ __forceinline__ void weights(f4_t* s, int n, float lv, float ref) {
+  __device__ __forceinline__ void weights(f4_t* s, int n, Linear s_of, float lv, float ref) {
     float top = s[0][0];
 #pragma unroll
     for (int t = 0; t < n; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
-    top = join_groups(top, Max()) + lv;
+    top = fmaf(join_groups(top, Max()), s_of.by, s_of.plus + lv);
     const float now = fmaxf(m, top), base = now == -INFINITY ? 0.f : now;
-    const float was = __builtin_amdgcn_exp2f(m - base), off = lv - base + kShift;
+    const float was = __builtin_amdgcn_exp2f(m - base), off = s_of.plus + lv - base + kShift;
     float sum = 0.f;
 #pragma unroll
     for (int t = 0; t < n; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[t][i] = __builtin_amdgcn_exp2f(s[t][i] + off);
+        s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], s_of.by, off));
         sum += s[t][i];
       }
     l = l * was + join_groups(sum, Add()) * __builtin_amdgcn_exp2f(fminf(fmaxf(ref - lv, -100.f), 100.f));
@@ -102,23 +102,23 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Score
   // (a block that is not there: any page's bytes, and none of its tokens seen)
   u4_t kw[8][F::kChunks], vw[F::kTiles][2];
   float ks, vs;
-  const size_t lane_k = (16 * (f.col >> 2) + (f.col & 3)) * D + 16 * f.grp, lane_v = f.col * kBlock + 16 * f.grp;
+  const uint32_t lane_k = (16 * (f.col >> 2) + (f.col & 3)) * D + 16 * f.grp, lane_v = f.col * kBlock + 16 * f.grp;
   auto request_k = [&](int page) {
     const size_t unit = (size_t)max(page, 0) * s.n_kv_heads + h;
-    const uint8_t* kc = s.k_codes + unit * (kBlock * D) + lane_k;
+    const uint8_t* kc = s.k_codes + unit * (kBlock * D);
 #pragma unroll
     for (int t = 0; t < 8; ++t)
 #pragma unroll
-      for (int p = 0; p < F::kChunks; ++p) kw[t][p] = *(const u4_t*)(kc + (64 * (t / 4) + 4 * (t % 4)) * D + 64 * p);
+      for (int p = 0; p < F::kChunks; ++p) kw[t][p] = *(const u4_t*)(kc + (64 * (t / 4) + 4 * (t % 4)) * D + 64 * p + lane_k);
     ks = scalar_scale(s.k_scales + unit);
   };
   auto request_v = [&](int page) {
     const size_t unit = (size_t)max(page, 0) * s.n_kv_heads + h;
-    const uint8_t* vc = s.v_codes + unit * (kBlock * D) + lane_v;
+    const uint8_t* vc = s.v_codes + unit * (kBlock * D);
 #pragma unroll
     for (int dt = 0; dt < F::kTiles; ++dt)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) vw[dt][u] = *(const u4_t*)(vc + 16 * dt * kBlock + 64 * u);
+      for (int u = 0; u < 2; ++u) vw[dt][u] = *(const u4_t*)(vc + 16 * dt * kBlock + 64 * u + lane_v);
     vs = scalar_scale(s.v_scales + unit);
   };
   f.m = -INFINITY;
@@ -136,8 +136,8 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Score
       shift = bf16_shift(__float_as_uint(join_groups(__uint_as_float(most), Max())));   // (bit patterns of positive numbers)
     }
 #pragma unroll
-    for (int k = 0; k < F::kSteps; ++k) f.q[k] = query8<ELEM>(raw[k], shift);
-    f.c = ldexpf(sc.scale, -shift);
+    for (int k = 0; k < F::kSteps; ++k) f.q[k] = query8<ELEM>(sc.scale < 0.f ? raw[k] ^ (uint16_t)0x8000 : raw[k], shift);
+    f.c = ldexpf(fabsf(sc.scale), -shift);   // (the queries have its sign)
   };
   if (begin < blocks.count) {
     int it = begin, page = blocks.pre == 0 && blocks.first == 0 && begin == guessed ? (guess < s.num_pages ? guess : -1) : page_in(s, table, blocks, begin);
@@ -166,10 +166,10 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Score
       }
     };
     auto outputs = [&]() {
-      finish_scores<f4_t, 8>(x, ck, sc, f.view, !all_seen(from, lo, hi, f.view.prefix, sc.window), from + 16 * f.grp,
+      const Linear s_of = finish_scores<f4_t, 8>(x, ck, sc, f.view, !all_seen(from, lo, hi, f.view.prefix, sc.window), from + 16 * f.grp,
                              [](int t, int i) { return 64 * (t / 4) + 4 * (t % 4) + i; });
       if (gone) no_scores<f4_t, 8>(x);
-      f.weights(x, 8, lv, ref);
+      f.weights(x, 8, s_of, lv, ref);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         h8_t p;
@@ -224,8 +224,10 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Score
           x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8_t, kx[t][k]), *(const bf8_t*)(q_row + 64 * (k / 2) + 16 * f.grp + 8 * (k % 2)), x[t], 0, 0, 0);
       }
     }
-    finish_scores<f4_t, 2>(x, sc.scale, sc, f.view, true, length - tail + first + 8 * f.grp, [](int t, int i) { return 4 * t + i; });
-    f.weights(x, 2, 0.f, ref);
+    if (ELEM == BD_ELEM_BF16 && sc.scale < 0.f)   // (f.q has its sign)
+      for (int t = 0; t < 2; ++t) x[t] = -x[t];
+    const Linear s_of = finish_scores<f4_t, 2>(x, fabsf(sc.scale), sc, f.view, true, length - tail + first + 8 * f.grp, [](int t, int i) { return 4 * t + i; });
+    f.weights(x, 2, s_of, 0.f, ref);
     if (ELEM == BD_ELEM_F16) {
       h8_t p;
 #pragma unroll

@@ -16,6 +16,7 @@ struct Parts8 {
 };
 hipError_t launch_kv8_few(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, void* ws, void* out,
                           hipStream_t st);
+constexpr int many_rows(int head_dim) { return head_dim == 64 ? 128 : 256; }   // of a workgroup of launch_kv8_many's
 hipError_t launch_kv8_many(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, float* part,
                            void* out, hipStream_t st);
 
