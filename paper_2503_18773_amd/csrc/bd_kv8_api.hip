@@ -104,8 +104,8 @@ Step8 step_of(const bd_paged8_cache* c, const int32_t* cu, int32_t total, int32_
 
 Rows8 rows_of(const bd_rows* r) { return r ? Rows8{(uint16_t*)r->data, r->token_stride, r->head_stride} : Rows8{nullptr, 0, 0}; }
 
-// Up to how many rows (tokens times query heads) of a KV head go by 16 against a block in a wave's registers, each 16 reading the
-// cache for itself; more are tiles of kManyRows that share blocks in LDS.
+// Up to how many rows (tokens times query heads) of a KV head go by 16 or 32 against a block in a wave's registers, each tile reading the
+// cache for itself; more are tiles of many_rows() that share blocks in LDS.
 constexpr long kFewRows = 64;
 
 }  // namespace
@@ -120,7 +120,7 @@ int kv8_splits(const bd_paged8_cache* c, int max_tokens, int max_len) {
   const long rows = (long)max_tokens * (c->n_q_heads / c->n_kv_heads);
   const long blocks = (std::max(max_len, 1) - 1L) / kBlock + 1;
   if (kv8_few(rows)) {
-    const long units = (long)c->batch * c->n_kv_heads * ((rows + 15) / 16);
+    const long units = (long)c->batch * c->n_kv_heads * few_tiles(rows);
     const long want = blocks <= 4 ? 1 : blocks <= 8 ? blocks : std::min(std::max(8L, blocks / 2), 64L);
     return (int)std::max(1L, std::min(want, 256 / units));
   }
@@ -199,7 +199,7 @@ int32_t bd_paged8_choose_splits(const bd_paged8_cache* c, int32_t max_tokens, in
 size_t bd_paged8_workspace_bytes(const bd_paged8_cache* c, int32_t total, int32_t max_tokens, int32_t num_splits) {
   if (check_shape8(c) != BD_OK || total < 1 || max_tokens < 1 || num_splits < 2) return 0;
   const long gq = c->n_q_heads / c->n_kv_heads;
-  auto few = [&](long rows) { return (size_t)std::min(num_splits, kMostSplits) * c->batch * c->n_kv_heads * ((rows + 15) / 16) * std::min(rows, 16L); };
+  auto few = [&](long rows) { return (size_t)std::min(num_splits, kMostSplits) * c->batch * c->n_kv_heads * few_tiles(rows) * std::min(rows, few_rows(rows)); };
   const long rows = std::min(max_tokens, total) * gq;
   size_t filed = kv8_few(rows) ? few(rows) : (size_t)num_splits * total * c->n_q_heads;
   if (kv8_few(gq)) filed = std::max(filed, few(gq));   // (a call without cu_tokens, whatever its max_tokens)
@@ -220,7 +220,7 @@ bd_status bd_paged8_attn(const bd_paged8_cache* c, const bd_rows* q, const int32
   const Step8 st = step_of(c, cu_tokens, total, max_tokens);
   const long rows = (long)st.max_tokens * st.gq;
   // launch grid dimensions: KV heads x tiles of rows, tiles x splits; the merge's rows
-  if (num_splits > 65535 || (kv8_few(rows) ? (rows + 15) / 16 * c->n_kv_heads : (rows + many_rows(c->head_dim) - 1) / many_rows(c->head_dim) * num_splits) > 65535 ||
+  if (num_splits > 65535 || (kv8_few(rows) ? few_tiles(rows) * c->n_kv_heads : (rows + many_rows(c->head_dim) - 1) / many_rows(c->head_dim) * num_splits) > 65535 ||
       ((long)st.max_tokens * c->n_q_heads + 3) / 4 > (1L << 24) - 1)
     return BD_ERR_UNSUPPORTED;
   const Scores8 sc{scores->softmax_scale, scores->softcap, scores->slopes, scores->prefix_lens, scores->window};

@@ -5,26 +5,26 @@
 namespace bd {
 namespace {
 
-// Sixteen rows (a token's query head each, token by token) of one KV head against blocks of 128 tokens, a wave a block.
+// Sixteen rows (a token's query head each, token by token), or twice that, of one KV head against blocks of 128 tokens, a wave a block.
 // Per block  S^T = K Q^T  and  O^T += V^T P^T  with 16 x 16 x 32 products, tokens x rows and channels x rows: a lane holds
-// scores and outputs of one row, and its scores are, as they come, the eight tokens that the second product wants of the lane.
+// scores and outputs of one row of each sixteen, and its scores are, as they come, the eight tokens that the second product wants of the lane.
 // The order of tokens inside of the products is free, and chosen so that a lane's codes are 16 adjacent bytes: S^T's row 4 a + i of
 // tile t is token 64 (t / 4) + 16 a + 4 (t % 4) + i, so lane group g has tokens 16 g .. 16 g + 15 of each half; likewise the channels of K.
 template <int D, int CODE, int ELEM>
 struct Few {
   static constexpr int kChunks = D / 64, kSteps = D / 32, kTiles = D / 16;
-  int lane, col, grp;
   h8_t q[kSteps];
   float c;       // scores in natural units per product and K scale
   RowView view;
   float m, l;    // running maximum (base 2, scale included) and sum of the lane's row
   f4_t acc[kTiles];
 
-  // weights in place of scores; lv: the block's V scale, ref: the reference scale, both as logarithms
-  __device__ __forceinline__ void weights(f4_t* s, int n, Linear s_of, float lv, float ref) {
+  // weights in place of N tiles' scores; lv: the block's V scale, ref: the reference scale, both as logarithms
+  template <int N>
+  __device__ __forceinline__ void weights(f4_t* s, Linear s_of, float lv, float ref) {
     float top = s[0][0];
 #pragma unroll
-    for (int t = 0; t < n; ++t)
+    for (int t = 0; t < N; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
     top = fmaf(join_groups(top, Max()), s_of.by, s_of.plus + lv);
@@ -32,7 +32,7 @@ struct Few {
     const float was = __builtin_amdgcn_exp2f(m - base), off = s_of.plus + lv - base + kShift;
     float sum = 0.f;
 #pragma unroll
-    for (int t = 0; t < n; ++t)
+    for (int t = 0; t < N; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         s[t][i] = __builtin_amdgcn_exp2f(fmaf(s[t][i], s_of.by, off));
@@ -60,13 +60,16 @@ __device__ __forceinline__ void get2(const float* p, float& a, float& b) {
 // The weight of a partial result, given the largest maximum.
 __device__ __forceinline__ float merge_weight(float m, float top) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top); }
 
-template <int D, int CODE, int ELEM>
-__global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Scores8 sc, int splits, Parts8 parts, uint16_t* out) {
+template <int D, int CODE, int ELEM, int NT>
+__global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Scores8 sc, int splits, int order, Parts8 parts, uint16_t* out) {
   typedef Few<D, CODE, ELEM> F;
-  constexpr int kPitch = D + 4;
-  __shared__ float lds[4 * 16 * kPitch + 4 * 16 * 2];
-  const int b = blockIdx.z, h = blockIdx.y % s.n_kv_heads, tile = blockIdx.y / s.n_kv_heads, split = blockIdx.x;
+  constexpr int kPitch = D + 4, kTileRows = 16 * NT;
+  __shared__ float lds[4 * kTileRows * kPitch + 4 * kTileRows * 2];
+  const int h = blockIdx.y % s.n_kv_heads, tile = blockIdx.y / s.n_kv_heads, split = blockIdx.x;
+  const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int before;
+  const int b = __builtin_amdgcn_readfirstlane(paged_sequence<false>(s.seq_lens, lane, before, order, 0, 0));
   // (requested with the length, for where the wave's first block turns out to be the one of that number)
   const int32_t* table = s.block_table + (size_t)b * s.max_pages;
   const int guessed = split + splits * wave;
@@ -74,27 +77,29 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Score
   Seq8 sq;
   if (!queries_of(s, b, sq)) return;
   const int rows = sq.n * s.gq;
-  if (16 * tile >= rows) return;
-  const int here = min(16, rows - 16 * tile);   // of the tile
-  F f;
-  f.lane = threadIdx.x & 63;
-  f.col = f.lane & 15;
-  f.grp = f.lane >> 4;
-  const int row = min(16 * tile + f.col, rows - 1), token = row / s.gq, head = h * s.gq + row % s.gq;
-  const int length = sq.len + sq.n, lo = sq.len + 16 * tile / s.gq, hi = sq.len + min(16 * tile + 15, rows - 1) / s.gq;
-  f.view.pos = sq.len + token;
-  f.view.prefix = sc.prefix ? min(max(scalar_load(sc.prefix + b), 0), length) : 0;
-  f.view.window = window_of(sc.window);
-  f.view.slope = sc.slopes ? sc.slopes[head] : 0.f;
-  const uint16_t* q_row = q.data + (sq.row + token) * q.token + head * q.head;
-  us8_t raw[F::kSteps];
+  if (kTileRows * tile >= rows) return;
+  const int here = min(kTileRows, rows - kTileRows * tile);   // of the tile
+  const int length = sq.len + sq.n, lo = sq.len + kTileRows * tile / s.gq, hi = sq.len + min(kTileRows * tile + kTileRows - 1, rows - 1) / s.gq;
+  const int prefix = sc.prefix ? min(max(scalar_load(sc.prefix + b), 0), length) : 0;
+  F f[NT];
+  const uint16_t* q_row[NT];
+  us8_t raw[NT][F::kSteps];
 #pragma unroll
-  for (int k = 0; k < F::kSteps; ++k) raw[k] = *(const us8_t*)(q_row + 64 * (k / 2) + 16 * f.grp + 8 * (k % 2));
+  for (int n = 0; n < NT; ++n) {
+    const int row = min(kTileRows * tile + 16 * n + col, rows - 1), token = row / s.gq, head = h * s.gq + row % s.gq;
+    f[n].view.pos = sq.len + token;
+    f[n].view.prefix = prefix;
+    f[n].view.window = window_of(sc.window);
+    f[n].view.slope = sc.slopes ? sc.slopes[head] : 0.f;
+    q_row[n] = q.data + (sq.row + token) * q.token + head * q.head + 16 * grp;
+#pragma unroll
+    for (int k = 0; k < F::kSteps; ++k) raw[n][k] = *(const us8_t*)(q_row[n] + 64 * (k / 2) + 8 * (k % 2));
+  }
 
   // Blocks are dealt to the splits in turn, and a split's to its waves: a few blocks are one to a workgroup, on compute units of their own, since
   // one of those draws some 35 GB/s whatever it asks for.  The residual goes, 32 tokens a wave, where the next block would.  No more splits
   // than that are at work.
-  const Blocks blocks(lo, hi, length, f.view.prefix, sc.window, s.max_pages);
+  const Blocks blocks(lo, hi, length, prefix, sc.window, s.max_pages);
   const int active = max(1, min(splits, blocks.count + blocks.tail));
   if (split >= active) return;
   const int begin = split + active * wave;
@@ -102,7 +107,7 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Score
   // (a block that is not there: any page's bytes, and none of its tokens seen)
   u4_t kw[8][F::kChunks], vw[F::kTiles][2];
   float ks, vs;
-  const uint32_t lane_k = (16 * (f.col >> 2) + (f.col & 3)) * D + 16 * f.grp, lane_v = f.col * kBlock + 16 * f.grp;
+  const uint32_t lane_k = (16 * (col >> 2) + (col & 3)) * D + 16 * grp, lane_v = col * kBlock + 16 * grp;
   auto request_k = [&](int page) {
     const size_t unit = (size_t)max(page, 0) * s.n_kv_heads + h;
     const uint8_t* kc = s.k_codes + unit * (kBlock * D);
@@ -121,23 +126,29 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Score
       for (int u = 0; u < 2; ++u) vw[dt][u] = *(const u4_t*)(vc + 16 * dt * kBlock + 64 * u + lane_v);
     vs = scalar_scale(s.v_scales + unit);
   };
-  f.m = -INFINITY;
-  f.l = 0.f;
 #pragma unroll
-  for (int dt = 0; dt < F::kTiles; ++dt) f.acc[dt] = f4_t{0.f, 0.f, 0.f, 0.f};
+  for (int n = 0; n < NT; ++n) {
+    f[n].m = -INFINITY;
+    f[n].l = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < F::kTiles; ++dt) f[n].acc[dt] = f4_t{0.f, 0.f, 0.f, 0.f};
+  }
   float ref;
   auto prepare = [&]() {   // (behind the first requests)
     ref = scale_reference(s, table, blocks, h);
-    int shift = 0;
-    if (ELEM == BD_ELEM_BF16) {
-      uint32_t most = 0;
 #pragma unroll
-      for (int k = 0; k < F::kSteps; ++k) most = max(most, most_of(raw[k]));
-      shift = bf16_shift(__float_as_uint(join_groups(__uint_as_float(most), Max())));   // (bit patterns of positive numbers)
+    for (int n = 0; n < NT; ++n) {
+      int shift = 0;
+      if (ELEM == BD_ELEM_BF16) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int k = 0; k < F::kSteps; ++k) most = max(most, most_of(raw[n][k]));
+        shift = bf16_shift(__float_as_uint(join_groups(__uint_as_float(most), Max())));   // (bit patterns of positive numbers)
+      }
+#pragma unroll
+      for (int k = 0; k < F::kSteps; ++k) f[n].q[k] = query8<ELEM>(sc.scale < 0.f ? raw[n][k] ^ (uint16_t)0x8000 : raw[n][k], shift);
+      f[n].c = ldexpf(fabsf(sc.scale), -shift);   // (the queries have its sign)
     }
-#pragma unroll
-    for (int k = 0; k < F::kSteps; ++k) f.q[k] = query8<ELEM>(sc.scale < 0.f ? raw[k] ^ (uint16_t)0x8000 : raw[k], shift);
-    f.c = ldexpf(fabsf(sc.scale), -shift);   // (the queries have its sign)
   };
   if (begin < blocks.count) {
     int it = begin, page = blocks.pre == 0 && blocks.first == 0 && begin == guessed ? (guess < s.num_pages ? guess : -1) : page_in(s, table, blocks, begin);
@@ -145,39 +156,53 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Score
     request_v(page);
     int next_page = page_in(s, table, blocks, it + 4 * active);
     prepare();
-    f4_t x[8];
+    f4_t x[NT][8];
     int from;
-    float ck, lv;
+    float block_k, lv;
     bool gone;
     auto products = [&]() {
       from = blocks[it] * kBlock;
       gone = page < 0;
       missing |= gone;
-      ck = f.c * ks;
+      block_k = ks;
       lv = vs > 0.f ? log2f(vs) : ref;
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        x[t] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int n = 0; n < NT; ++n) x[n][t] = f4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int p = 0; p < F::kChunks; ++p) {
-          x[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<CODE>(kw[t][p][0], kw[t][p][1]), f.q[2 * p], x[t], 0, 0, 0);
-          x[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<CODE>(kw[t][p][2], kw[t][p][3]), f.q[2 * p + 1], x[t], 0, 0, 0);
+          const h8_t k0 = codes8<CODE>(kw[t][p][0], kw[t][p][1]), k1 = codes8<CODE>(kw[t][p][2], kw[t][p][3]);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            x[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, f[n].q[2 * p], x[n][t], 0, 0, 0);
+            x[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, f[n].q[2 * p + 1], x[n][t], 0, 0, 0);
+          }
         }
       }
     };
     auto outputs = [&]() {
-      const Linear s_of = finish_scores<f4_t, 8>(x, ck, sc, f.view, !all_seen(from, lo, hi, f.view.prefix, sc.window), from + 16 * f.grp,
-                             [](int t, int i) { return 64 * (t / 4) + 4 * (t % 4) + i; });
-      if (gone) no_scores<f4_t, 8>(x);
-      f.weights(x, 8, s_of, lv, ref);
+      const bool masked = !all_seen(from, lo, hi, prefix, sc.window);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const Linear s_of = finish_scores<f4_t, 8>(x[n], f[n].c * block_k, sc, f[n].view, masked, from + 16 * grp,
+                                                   [](int t, int i) { return 64 * (t / 4) + 4 * (t % 4) + i; });
+        if (gone) no_scores<f4_t, 8>(x[n]);
+        f[n].template weights<8>(x[n], s_of, lv, ref);
+      }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        h8_t p;
+        h8_t p[NT];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = (_Float16)x[2 * k + e / 4][e % 4];
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int dt = 0; dt < F::kTiles; ++dt)
-          f.acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes8<CODE>(vw[dt][k / 2][2 * (k % 2)], vw[dt][k / 2][2 * (k % 2) + 1]), p, f.acc[dt], 0, 0, 0);
+          for (int e = 0; e < 8; ++e) p[n][e] = (_Float16)x[n][2 * k + e / 4][e % 4];
+#pragma unroll
+        for (int dt = 0; dt < F::kTiles; ++dt) {
+          const h8_t v = codes8<CODE>(vw[dt][k / 2][2 * (k % 2)], vw[dt][k / 2][2 * (k % 2) + 1]);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) f[n].acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[n], f[n].acc[dt], 0, 0, 0);
+        }
       }
     };
     // The next block's keys are on their way while the scores and values are dealt with, its values behind them.  (The last block is
@@ -196,13 +221,13 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Score
   } else {
     prepare();
   }
-  if (missing && s.status && f.lane == 0) atomicOr(s.status, kStatusRead);
+  if (missing && s.status && lane == 0) atomicOr(s.status, kStatusRead);
 
   const int tail = length % kBlock, first = 32 * wave;
   if (blocks.tail && split == blocks.count % active && first < tail) {
     const size_t unit = (size_t)b * s.n_kv_heads + h;
-    const uint16_t* kr = s.k_res + unit * (kBlock * D) + (first + 8 * (f.col >> 2) + (f.col & 3)) * D + 16 * f.grp;
-    const uint16_t* vr = s.v_res + unit * (kBlock * D) + (first + 8 * f.grp) * D + f.col;
+    const uint16_t* kr = s.k_res + unit * (kBlock * D) + (first + 8 * (col >> 2) + (col & 3)) * D + 16 * grp;
+    const uint16_t* vr = s.v_res + unit * (kBlock * D) + (first + 8 * grp) * D + col;
     us8_t kx[2][F::kSteps], vx[F::kTiles];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -211,96 +236,103 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Score
 #pragma unroll
     for (int dt = 0; dt < F::kTiles; ++dt)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) vx[dt][e] = first + 8 * f.grp + e < tail ? vr[e * D + 16 * dt] : (uint16_t)0;   // (rows behind the last are anything)
-    f4_t x[2];
+      for (int e = 0; e < 8; ++e) vx[dt][e] = first + 8 * grp + e < tail ? vr[e * D + 16 * dt] : (uint16_t)0;   // (rows behind the last are anything)
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      x[t] = f4_t{0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < NT; ++n) {
+      f4_t x[2];
 #pragma unroll
-      for (int k = 0; k < F::kSteps; ++k) {
-        if (ELEM == BD_ELEM_F16)
-          x[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, kx[t][k]), f.q[k], x[t], 0, 0, 0);
-        else
-          x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8_t, kx[t][k]), *(const bf8_t*)(q_row + 64 * (k / 2) + 16 * f.grp + 8 * (k % 2)), x[t], 0, 0, 0);
+      for (int t = 0; t < 2; ++t) {
+        x[t] = f4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < F::kSteps; ++k) {
+          if (ELEM == BD_ELEM_F16)
+            x[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, kx[t][k]), f[n].q[k], x[t], 0, 0, 0);
+          else
+            x[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8_t, kx[t][k]), *(const bf8_t*)(q_row[n] + 64 * (k / 2) + 8 * (k % 2)), x[t], 0, 0, 0);
+        }
+        if (ELEM == BD_ELEM_BF16 && sc.scale < 0.f) x[t] = -x[t];   // (f.q has its sign)
       }
-    }
-    if (ELEM == BD_ELEM_BF16 && sc.scale < 0.f)   // (f.q has its sign)
-      for (int t = 0; t < 2; ++t) x[t] = -x[t];
-    const Linear s_of = finish_scores<f4_t, 2>(x, fabsf(sc.scale), sc, f.view, true, length - tail + first + 8 * f.grp, [](int t, int i) { return 4 * t + i; });
-    f.weights(x, 2, s_of, 0.f, ref);
-    if (ELEM == BD_ELEM_F16) {
+      const Linear s_of = finish_scores<f4_t, 2>(x, fabsf(sc.scale), sc, f[n].view, true, length - tail + first + 8 * grp, [](int t, int i) { return 4 * t + i; });
+      f[n].template weights<2>(x, s_of, 0.f, ref);
       h8_t p;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = (_Float16)x[e / 4][e % 4];
-#pragma unroll
-      for (int dt = 0; dt < F::kTiles; ++dt)
-        f.acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, vx[dt]), p, f.acc[dt], 0, 0, 0);
-    } else {
-      // bf16 values want bf16 weights: in two pieces, 16 bits of them
-      bf8_t p, p2;
+      bf8_t p1, p2;   // bf16 values want bf16 weights: in two pieces, 16 bits of them
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        p[e] = (__bf16)x[e / 4][e % 4];
-        p2[e] = (__bf16)(x[e / 4][e % 4] - (float)p[e]);
+        const float y = x[e / 4][e % 4];
+        p[e] = (_Float16)y;
+        p1[e] = (__bf16)y;
+        p2[e] = (__bf16)(y - (float)p1[e]);
       }
 #pragma unroll
       for (int dt = 0; dt < F::kTiles; ++dt) {
-        f.acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8_t, vx[dt]), p, f.acc[dt], 0, 0, 0);
-        f.acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8_t, vx[dt]), p2, f.acc[dt], 0, 0, 0);
+        if (ELEM == BD_ELEM_F16) {
+          f[n].acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, vx[dt]), p, f[n].acc[dt], 0, 0, 0);
+        } else {
+          f[n].acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8_t, vx[dt]), p1, f[n].acc[dt], 0, 0, 0);
+          f[n].acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8_t, vx[dt]), p2, f[n].acc[dt], 0, 0, 0);
+        }
       }
     }
   }
 
   // the four waves' results, in units of 2^(m - kShift) and, the sums, of 2^ref
-  float* ml = lds + 4 * 16 * kPitch;
-  if (f.col < here) {
-    if (f.grp == 0) {
-      ml[(wave * 16 + f.col) * 2] = f.m;
-      ml[(wave * 16 + f.col) * 2 + 1] = f.l;
-    }
+  float* ml = lds + 4 * kTileRows * kPitch;
 #pragma unroll
-    for (int dt = 0; dt < F::kTiles; ++dt) *(f4_t*)(lds + (wave * 16 + f.col) * kPitch + 16 * dt + 4 * f.grp) = f.acc[dt];
+  for (int n = 0; n < NT; ++n) {
+    const int r = 16 * n + col;
+    if (r < here) {
+      if (grp == 0) {
+        ml[(wave * kTileRows + r) * 2] = f[n].m;
+        ml[(wave * kTileRows + r) * 2 + 1] = f[n].l;
+      }
+#pragma unroll
+      for (int dt = 0; dt < F::kTiles; ++dt) *(f4_t*)(lds + (wave * kTileRows + r) * kPitch + 16 * dt + 4 * grp) = f[n].acc[dt];
+    }
   }
   __syncthreads();
   constexpr int kPer = D / 16;   // channels a thread
-  const int r = threadIdx.x / 16, d = threadIdx.x % 16 * kPer;
+  const int d = threadIdx.x % 16 * kPer;
   const float unit = __builtin_amdgcn_exp2f(ref);
-  float o[kPer] = {}, sum = 0.f, top = -INFINITY;
-  if (r < here) {
+  const int units = s.batch * (int)gridDim.y, at = b * (int)gridDim.y + blockIdx.y;
+  const int filed = min(kTileRows, s.max_tokens * s.gq);   // rows of a partial result
+  float* po = parts.data + (size_t)at * splits * filed * D;
+  float* pml = parts.data + (size_t)units * splits * filed * D + (size_t)at * splits * filed * 2;
+  auto to_out = [&](int r, const float* o, float sum) {
+    const int i = kTileRows * tile + r;
+    const size_t out_row = sq.row * (size_t)s.n_q_heads + (size_t)(i / s.gq) * s.n_q_heads + h * s.gq + i % s.gq;
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[(w * 16 + r) * 2]);
+    for (int e = 0; e < kPer; e += 2) *(uint32_t*)(out + out_row * D + d + e) = elem2<ELEM>(o[e] * inv, o[e + 1] * inv);
+  };
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int r = 16 * n + threadIdx.x / 16;
+    if (r >= here) continue;
+    float o[kPer] = {}, sum = 0.f, top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[(w * kTileRows + r) * 2]);
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float fac = merge_weight(ml[(w * 16 + r) * 2], top);
-      sum += fac * ml[(w * 16 + r) * 2 + 1];
+      const float fac = merge_weight(ml[(w * kTileRows + r) * 2], top);
+      sum += fac * ml[(w * kTileRows + r) * 2 + 1];
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) o[e] += fac * lds[(w * 16 + r) * kPitch + d + e];
+      for (int e = 0; e < kPer; ++e) o[e] += fac * lds[(w * kTileRows + r) * kPitch + d + e];
     }
 #pragma unroll
     for (int e = 0; e < kPer; ++e) o[e] *= unit;
-  }
-  const size_t token_row = sq.row * (size_t)s.n_q_heads;
-  auto out_row = [&](int i) { return token_row + (size_t)((16 * tile + i) / s.gq) * s.n_q_heads + h * s.gq + (16 * tile + i) % s.gq; };
-  if (active == 1) {
-    if (r >= here) return;
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    if (active == 1) {
+      to_out(r, o, sum);
+    } else {
 #pragma unroll
-    for (int e = 0; e < kPer; e += 2) *(uint32_t*)(out + out_row(r) * D + d + e) = elem2<ELEM>(o[e] * inv, o[e + 1] * inv);
-    return;
+      for (int e = 0; e < kPer; e += 2) put2(po + (split * filed + r) * D + d + e, o[e], o[e + 1]);
+      if (d == 0) put2(pml + (split * filed + r) * 2, top, sum);
+    }
   }
+  if (active == 1) return;
 
   // The workgroup that files the last of the partial results merges them, which spares a launch.  They pass between XCDs, whose L2
   // caches do not know of each other: device-scope stores and loads, which go through those, so that no cache has to be written back or emptied
   // (as a release and an acquire at that scope would); a store is waited for before it is counted.
-  const int units = s.batch * (int)gridDim.y, at = b * (int)gridDim.y + blockIdx.y;
-  const int filed = min(16, s.max_tokens * s.gq);   // rows of a partial result
-  float* po = parts.data + (size_t)at * splits * filed * D;
-  float* pml = parts.data + (size_t)units * splits * filed * D + (size_t)at * splits * filed * 2;
-  if (r < here) {
-#pragma unroll
-    for (int e = 0; e < kPer; e += 2) put2(po + (split * filed + r) * D + d + e, o[e], o[e + 1]);
-    if (d == 0) put2(pml + (split * filed + r) * 2, top, sum);
-  }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   uint32_t* seen = (uint32_t*)lds;
@@ -311,91 +343,103 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Score
   }
   __syncthreads();
   if (*seen != (uint32_t)active) return;
-  __syncthreads();
-  // outputs: rows x slices of the splits fill the workgroup; a thread's first ones are on their way with the maxima and sums
-  const int held = here > 8 ? 16 : here > 4 ? 8 : here > 2 ? 4 : here, slices = 16 / held, mr = r % held, slice = r / held;
-  constexpr int kAhead = 8;
-  float ahead[kAhead][kPer];
-#pragma unroll
-  for (int i = 0; i < kAhead; ++i)
-#pragma unroll
-    for (int e = 0; e < kPer; e += 2) {
-      ahead[i][e] = ahead[i][e + 1] = 0.f;
-      if (slice + i * slices < active && mr < here) get2(po + ((slice + i * slices) * filed + mr) * D + d + e, ahead[i][e], ahead[i][e + 1]);
-    }
-  // a row's maxima and sums by 16 threads
   float* fac = lds;                            // [16][kMostSplits] weights of the partial results
   float* sums = lds + 16 * kMostSplits;        // [16]
   float* slices_o = sums + 16;                 // [slice][row][D]
-  const int lane16 = threadIdx.x % 16;
-  float all = -INFINITY, mm[kMostSplits / 16], ll[kMostSplits / 16];
+  for (int n = 0; n < NT && 16 * n < here; ++n) {
+    __syncthreads();
+    const int r = threadIdx.x / 16, left = min(16, here - 16 * n);
+    const float* from_o = po + 16 * n * D;
+    const float* from_ml = pml + 16 * n * 2;
+    // outputs: rows x slices of the splits fill the workgroup; a thread's first ones are on their way with the maxima and sums
+    const int held = left > 8 ? 16 : left > 4 ? 8 : left > 2 ? 4 : left, slices = 16 / held, mr = r % held, slice = r / held;
+    constexpr int kAhead = 8;
+    float ahead[kAhead][kPer];
 #pragma unroll
-  for (int i = 0; i < kMostSplits / 16; ++i) {
-    mm[i] = -INFINITY;
-    ll[i] = 0.f;
-    if (16 * i + lane16 < active && r < here) get2(pml + ((16 * i + lane16) * filed + r) * 2, mm[i], ll[i]);
-    all = fmaxf(all, mm[i]);
-  }
-#pragma unroll
-  for (int x = 1; x < 16; x *= 2) all = fmaxf(all, __shfl_xor(all, x));
-  float l = 0.f;
-#pragma unroll
-  for (int i = 0; i < kMostSplits / 16; ++i) {
-    const float w = merge_weight(mm[i], all);
-    l += w * ll[i];
-    fac[r * kMostSplits + 16 * i + lane16] = w;
-  }
-#pragma unroll
-  for (int x = 1; x < 16; x *= 2) l += __shfl_xor(l, x);
-  if (lane16 == 0) sums[r] = l;
-  __syncthreads();
-  float acc[kPer] = {};
-  if (mr < here) {
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      if (slice + i * slices >= active) break;
-      const float w = fac[mr * kMostSplits + slice + i * slices];
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) acc[e] += w * ahead[i][e];
-    }
-#pragma unroll 8
-    for (int k = slice + kAhead * slices; k < active; k += slices) {
-      const float w = fac[mr * kMostSplits + k];
+    for (int i = 0; i < kAhead; ++i)
 #pragma unroll
       for (int e = 0; e < kPer; e += 2) {
-        float y0, y1;
-        get2(po + (k * filed + mr) * D + d + e, y0, y1);
-        acc[e] += w * y0;
-        acc[e + 1] += w * y1;
+        ahead[i][e] = ahead[i][e + 1] = 0.f;
+        if (slice + i * slices < active && mr < left) get2(from_o + ((slice + i * slices) * filed + mr) * D + d + e, ahead[i][e], ahead[i][e + 1]);
+      }
+    // a row's maxima and sums by 16 threads
+    const int lane16 = threadIdx.x % 16;
+    float all = -INFINITY, mm[kMostSplits / 16], ll[kMostSplits / 16];
+#pragma unroll
+    for (int i = 0; i < kMostSplits / 16; ++i) {
+      mm[i] = -INFINITY;
+      ll[i] = 0.f;
+      if (16 * i + lane16 < active && r < left) get2(from_ml + ((16 * i + lane16) * filed + r) * 2, mm[i], ll[i]);
+      all = fmaxf(all, mm[i]);
+    }
+#pragma unroll
+    for (int x = 1; x < 16; x *= 2) all = fmaxf(all, __shfl_xor(all, x));
+    float l = 0.f;
+#pragma unroll
+    for (int i = 0; i < kMostSplits / 16; ++i) {
+      const float w = merge_weight(mm[i], all);
+      l += w * ll[i];
+      fac[r * kMostSplits + 16 * i + lane16] = w;
+    }
+#pragma unroll
+    for (int x = 1; x < 16; x *= 2) l += __shfl_xor(l, x);
+    if (lane16 == 0) sums[r] = l;
+    __syncthreads();
+    float acc[kPer] = {};
+    if (mr < left) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (slice + i * slices >= active) break;
+        const float w = fac[mr * kMostSplits + slice + i * slices];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[e] += w * ahead[i][e];
+      }
+#pragma unroll 8
+      for (int k = slice + kAhead * slices; k < active; k += slices) {
+        const float w = fac[mr * kMostSplits + k];
+#pragma unroll
+        for (int e = 0; e < kPer; e += 2) {
+          float y0, y1;
+          get2(from_o + (k * filed + mr) * D + d + e, y0, y1);
+          acc[e] += w * y0;
+          acc[e + 1] += w * y1;
+        }
       }
     }
+#pragma unroll
+    for (int e = 0; e < kPer; e += 4) *(f4_t*)(slices_o + r * kPitch + d + e) = f4_t{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+    __syncthreads();
+    if (r < left) {
+      float o[kPer] = {};
+      for (int k = 0; k < slices; ++k)
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] += slices_o[(k * held + r) * kPitch + d + e];
+      to_out(16 * n + r, o, sums[r]);
+    }
   }
-#pragma unroll
-  for (int e = 0; e < kPer; e += 4) *(f4_t*)(slices_o + r * kPitch + d + e) = f4_t{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
-  __syncthreads();
-  if (r >= here) return;
-#pragma unroll
-  for (int e = 0; e < kPer; ++e) o[e] = 0.f;
-  for (int k = 0; k < slices; ++k)
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) o[e] += slices_o[(k * held + r) * kPitch + d + e];
-  const float inv = sums[r] > 0.f ? 1.f / sums[r] : 0.f;
-#pragma unroll
-  for (int e = 0; e < kPer; e += 2) *(uint32_t*)(out + out_row(r) * D + d + e) = elem2<ELEM>(o[e] * inv, o[e + 1] * inv);
 }
 
 }  // namespace
 
 hipError_t launch_kv8_few(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, void* ws, void* out,
                           hipStream_t st) {
-  const long tiles = ((long)s.max_tokens * s.gq + 15) / 16;
+  const long rows = (long)s.max_tokens * s.gq, tiles = few_tiles(rows);
   if (s.n_kv_heads * tiles * s.batch > kCounters) splits = 1;   // (far more workgroups than the chip holds)
   splits = splits < kMostSplits ? splits : kMostSplits;
   const Parts8 parts{(uint32_t*)ws, (float*)((char*)ws + BD_PAGED8_COUNTER_BYTES)};
   const dim3 grid(splits, (unsigned)(s.n_kv_heads * tiles), s.batch);
-#define BD_RUN(D, C, E) hipLaunchKernelGGL((kv8_few_kernel<D, C, E>), grid, dim3(256), 0, st, s, q, sc, splits, parts, (uint16_t*)out)
+  // (more workgroups than compute units: the longest sequences first)
+  const int order = s.batch >= 2 && s.batch <= 64 && (long)splits * s.n_kv_heads * tiles * s.batch > 256 ? s.batch : 0;
+#define BD_RUN_N(D, C, E, N) \
+  hipLaunchKernelGGL((kv8_few_kernel<D, C, E, N>), grid, dim3(256), 0, st, s, q, sc, splits, order, parts, (uint16_t*)out)
+#define BD_RUN(D, C, E)                       \
+  do {                                        \
+    if (rows <= 16) BD_RUN_N(D, C, E, 1);     \
+    else BD_RUN_N(D, C, E, 2);                \
+  } while (0)
   BD_KV8_INSTANCES(head_dim, code, elem, BD_RUN)
 #undef BD_RUN
+#undef BD_RUN_N
   return hipGetLastError();
 }
 

@@ -6,10 +6,12 @@
 namespace bd {
 
 // Few rows: the launch merges its splits' partial results itself, in up to kMostSplits of them, with a counter for each of up to
-// kCounters units (sequence, KV head, tile of 16 rows).  Workspace: the counters, then [unit][split][rows][D] unnormalised outputs and [unit][split]
+// kCounters units (sequence, KV head, tile of 16 rows, or 32 where a sequence may have more than 16).  Workspace: the counters, then [unit][split][rows][D] unnormalised outputs and [unit][split]
 // [rows][2] maxima (base 2) and sums.
 constexpr int kMostSplits = 128;
 constexpr long kCounters = BD_PAGED8_COUNTER_BYTES / 4;
+constexpr long few_rows(long rows) { return rows <= 16 ? 16 : 32; }   // of a tile
+constexpr long few_tiles(long rows) { return (rows + few_rows(rows) - 1) / few_rows(rows); }
 struct Parts8 {
   uint32_t* counters;
   float* data;
