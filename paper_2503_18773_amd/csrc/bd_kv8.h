@@ -22,6 +22,19 @@ struct Step8 {
   int batch, n_q_heads, n_kv_heads, gq, num_pages, max_pages, total, max_tokens;
 };
 
+// What a workgroup's first loads wait for, as scalars ahead of a kernel's structures: those are in registers when it starts
+// (build.py), the structures have to be fetched first.
+#define BD_KV8_HOT_PARAMS \
+  const int32_t *hot_table, const int32_t *hot_lens, const int32_t *hot_cu, int hot_max_pages, int hot_total, int hot_max_tokens
+#define BD_KV8_HOT_ARGS(s) (s).block_table, (s).seq_lens, (s).cu, (s).max_pages, (s).total, (s).max_tokens
+#define BD_KV8_HOT(s)                             \
+  (s).block_table = hot_table;                    \
+  (s).seq_lens = const_cast<int32_t*>(hot_lens);  \
+  (s).cu = hot_cu;                                \
+  (s).max_pages = hot_max_pages;                  \
+  (s).total = hot_total;                          \
+  (s).max_tokens = hot_max_tokens
+
 struct Rotate8 {
   const float* table;
   const int32_t* positions;

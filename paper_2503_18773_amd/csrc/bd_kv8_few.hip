@@ -61,7 +61,8 @@ __device__ __forceinline__ void get2(const float* p, float& a, float& b) {
 __device__ __forceinline__ float merge_weight(float m, float top) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top); }
 
 template <int D, int CODE, int ELEM, int NT>
-__global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Scores8 sc, int splits, int order, Parts8 parts, uint16_t* out) {
+__global__ __launch_bounds__(256, 1) void kv8_few_kernel(BD_KV8_HOT_PARAMS, int splits, int order, Step8 s, Rows8 q, Scores8 sc, Parts8 parts, uint16_t* out) {
+  BD_KV8_HOT(s);
   typedef Few<D, CODE, ELEM> F;
   constexpr int kPitch = D + 4, kTileRows = 16 * NT;
   __shared__ float lds[4 * kTileRows * kPitch + 4 * kTileRows * 2];
@@ -150,6 +151,22 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Score
       f[n].c = ldexpf(fabsf(sc.scale), -shift);   // (the queries have its sign)
     }
   };
+  const int tail = length % kBlock, first = 32 * wave;
+  const bool rest = blocks.tail && split == blocks.count % active && first < tail;
+  us8_t kx[2][F::kSteps], vx[F::kTiles];
+  auto request_rest = [&]() {
+    const size_t unit = ((size_t)b * s.n_kv_heads + h) * (kBlock * D);
+    const uint16_t* kr = s.k_res + unit + (first + 8 * (col >> 2) + (col & 3)) * D + 16 * grp;
+    const uint16_t* vr = s.v_res + unit + (first + 8 * grp) * D + col;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int k = 0; k < F::kSteps; ++k) kx[t][k] = *(const us8_t*)(kr + 4 * t * D + 64 * (k / 2) + 8 * (k % 2));
+#pragma unroll
+    for (int dt = 0; dt < F::kTiles; ++dt)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) vx[dt][e] = first + 8 * grp + e < tail ? vr[e * D + 16 * dt] : (uint16_t)0;   // (rows behind the last are anything)
+  };
   if (begin < blocks.count) {
     int it = begin, page = blocks.pre == 0 && blocks.first == 0 && begin == guessed ? (guess < s.num_pages ? guess : -1) : page_in(s, table, blocks, begin);
     request_k(page);
@@ -218,25 +235,14 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(Step8 s, Rows8 q, Score
       products();
     }
     outputs();
+    if (rest) request_rest();
   } else {
+    if (rest) request_rest();
     prepare();
   }
   if (missing && s.status && lane == 0) atomicOr(s.status, kStatusRead);
 
-  const int tail = length % kBlock, first = 32 * wave;
-  if (blocks.tail && split == blocks.count % active && first < tail) {
-    const size_t unit = (size_t)b * s.n_kv_heads + h;
-    const uint16_t* kr = s.k_res + unit * (kBlock * D) + (first + 8 * (col >> 2) + (col & 3)) * D + 16 * grp;
-    const uint16_t* vr = s.v_res + unit * (kBlock * D) + (first + 8 * grp) * D + col;
-    us8_t kx[2][F::kSteps], vx[F::kTiles];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int k = 0; k < F::kSteps; ++k) kx[t][k] = *(const us8_t*)(kr + 4 * t * D + 64 * (k / 2) + 8 * (k % 2));
-#pragma unroll
-    for (int dt = 0; dt < F::kTiles; ++dt)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) vx[dt][e] = first + 8 * grp + e < tail ? vr[e * D + 16 * dt] : (uint16_t)0;   // (rows behind the last are anything)
+  if (rest) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       f4_t x[2];
@@ -431,7 +437,7 @@ hipError_t launch_kv8_few(const Step8& s, int head_dim, int code, int elem, cons
   // (more workgroups than compute units: the longest sequences first)
   const int order = s.batch >= 2 && s.batch <= 64 && (long)splits * s.n_kv_heads * tiles * s.batch > 256 ? s.batch : 0;
 #define BD_RUN_N(D, C, E, N) \
-  hipLaunchKernelGGL((kv8_few_kernel<D, C, E, N>), grid, dim3(256), 0, st, s, q, sc, splits, order, parts, (uint16_t*)out)
+  hipLaunchKernelGGL((kv8_few_kernel<D, C, E, N>), grid, dim3(256), 0, st, BD_KV8_HOT_ARGS(s), splits, order, s, q, sc, parts, (uint16_t*)out)
 #define BD_RUN(D, C, E)                       \
   do {                                        \
     if (rows <= 16) BD_RUN_N(D, C, E, 1);     \
