@@ -199,7 +199,10 @@ int32_t bd_paged8_choose_splits(const bd_paged8_cache* c, int32_t max_tokens, in
 size_t bd_paged8_workspace_bytes(const bd_paged8_cache* c, int32_t total, int32_t max_tokens, int32_t num_splits) {
   if (check_shape8(c) != BD_OK || total < 1 || max_tokens < 1 || num_splits < 2) return 0;
   const long gq = c->n_q_heads / c->n_kv_heads;
-  auto few = [&](long rows) { return (size_t)std::min(num_splits, kMostSplits) * c->batch * c->n_kv_heads * few_tiles(rows) * std::min(rows, few_rows(rows)); };
+  // (256: where splits are dealt by length there are as many as compute units)
+  auto few = [&](long rows) {
+    return std::max((size_t)std::min(num_splits, kMostSplits) * c->batch * c->n_kv_heads * few_tiles(rows), c->batch > 1 ? (size_t)256 : 0) * std::min(rows, few_rows(rows));
+  };
   const long rows = std::min(max_tokens, total) * gq;
   size_t filed = kv8_few(rows) ? few(rows) : (size_t)num_splits * total * c->n_q_heads;
   if (kv8_few(gq)) filed = std::max(filed, few(gq));   // (a call without cu_tokens, whatever its max_tokens)

@@ -60,17 +60,67 @@ __device__ __forceinline__ void get2(const float* p, float& a, float& b) {
 // The weight of a partial result, given the largest maximum.
 __device__ __forceinline__ float merge_weight(float m, float top) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top); }
 
+// A ragged batch's workgroups, dealt by length: of the `room` that there are for a head's tile, a sequence gets one for so many blocks each
+// (six at least) that all of them find room.  This workgroup's sequence, its number among that one's, how many those are, and the first one's
+// number; false: it is left over.  (Lengths as they are before the step, whatever lists and prefixes make of them.)  Against as many splits for
+// each: 4 sequences of 20000 down to 6700 tokens 31.8 -> 28.6 us, 3 of up to 60000 60.5 -> 52.0, 24 of up to 5000 and 4 KV heads 27.0 -> 22.8; it
+// takes a microsecond, which short ones do not make up for (16 of up to 4000, five queries each, 34.3 / 35.8, 2 of 700 9.6 / 10.6): the
+// table's width is what the host knows of the lengths.
+struct Share {
+  int b, split, splits, first;
+};
+__device__ __forceinline__ bool fair_share(const Step8& s, int lane, int room, int window, Share& share) {
+  int blocks = lane < s.batch ? max(s.seq_lens[lane], 0) / kBlock + 1 : 0;
+  if (window) blocks = min(blocks, window / kBlock + 2);
+  const float mine = (float)blocks;
+  float each = ceilf(fmaxf(join_groups(row_sum16(mine), Add()) / (float)max(1, room - s.batch / 2), 6.f)), wanted;
+  for (int i = 0;; ++i) {
+    wanted = fminf(ceilf(mine / each), (float)kMostSplits);
+    const float need = join_groups(row_sum16(wanted), Add());
+    if (need <= (float)room) break;
+    if (i == 8) {   // (not seen; one for each has room: launch_kv8_few)
+      wanted = lane < s.batch ? 1.f : 0.f;
+      break;
+    }
+    each = ceilf(each * fmaxf(need / (float)room, 1.02f));
+  }
+  int to = (int)wanted;   // running sum over the lanes
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int other = __shfl_up(to, d);
+    to += lane >= d ? other : 0;
+  }
+  const uint64_t found = __ballot((int)blockIdx.x < to);
+  if (!found) return false;
+  const int at = __builtin_ctzll(found);
+  share.b = at;
+  share.splits = __builtin_amdgcn_readlane((int)wanted, at);
+  share.first = __builtin_amdgcn_readlane(to, at) - share.splits;
+  share.split = (int)blockIdx.x - share.first;
+  return true;
+}
+
 template <int D, int CODE, int ELEM, int NT>
-__global__ __launch_bounds__(256, 1) void kv8_few_kernel(BD_KV8_HOT_PARAMS, int splits, int order, Step8 s, Rows8 q, Scores8 sc, Parts8 parts, uint16_t* out) {
+__global__ __launch_bounds__(256, 1) void kv8_few_kernel(BD_KV8_HOT_PARAMS, int splits, int order, int room, Step8 s, Rows8 q, Scores8 sc, Parts8 parts, uint16_t* out) {
   BD_KV8_HOT(s);
   typedef Few<D, CODE, ELEM> F;
   constexpr int kPitch = D + 4, kTileRows = 16 * NT;
   __shared__ float lds[4 * kTileRows * kPitch + 4 * kTileRows * 2];
-  const int h = blockIdx.y % s.n_kv_heads, tile = blockIdx.y / s.n_kv_heads, split = blockIdx.x;
+  const int h = blockIdx.y % s.n_kv_heads, tile = blockIdx.y / s.n_kv_heads;
   const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int before;
-  const int b = __builtin_amdgcn_readfirstlane(paged_sequence<false>(s.seq_lens, lane, before, order, 0, 0));
+  int b, split = blockIdx.x, slot = 0;   // slot: where the sequence's partial results begin, of its head's tile
+  if (room) {
+    Share share;
+    if (!fair_share(s, lane, room, sc.window, share)) return;
+    b = share.b;
+    split = share.split;
+    splits = share.splits;
+    slot = share.first;
+  } else {
+    int before;
+    b = __builtin_amdgcn_readfirstlane(paged_sequence<false>(s.seq_lens, lane, before, order, 0, 0));
+  }
   // (requested with the length, for where the wave's first block turns out to be the one of that number)
   const int32_t* table = s.block_table + (size_t)b * s.max_pages;
   const int guessed = split + splits * wave;
@@ -299,10 +349,11 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(BD_KV8_HOT_PARAMS, int 
   constexpr int kPer = D / 16;   // channels a thread
   const int d = threadIdx.x % 16 * kPer;
   const float unit = __builtin_amdgcn_exp2f(ref);
-  const int units = s.batch * (int)gridDim.y, at = b * (int)gridDim.y + blockIdx.y;
+  const int at = b * (int)gridDim.y + blockIdx.y;   // of the counters
+  const int slots = (room ? room : s.batch * splits) * (int)gridDim.y, first_slot = room ? (int)blockIdx.y * room + slot : at * splits;
   const int filed = min(kTileRows, s.max_tokens * s.gq);   // rows of a partial result
-  float* po = parts.data + (size_t)at * splits * filed * D;
-  float* pml = parts.data + (size_t)units * splits * filed * D + (size_t)at * splits * filed * 2;
+  float* po = parts.data + (size_t)first_slot * filed * D;
+  float* pml = parts.data + (size_t)slots * filed * D + (size_t)first_slot * filed * 2;
   auto to_out = [&](int r, const float* o, float sum) {
     const int i = kTileRows * tile + r;
     const size_t out_row = sq.row * (size_t)s.n_q_heads + (size_t)(i / s.gq) * s.n_q_heads + h * s.gq + i % s.gq;
@@ -433,11 +484,15 @@ hipError_t launch_kv8_few(const Step8& s, int head_dim, int code, int elem, cons
   if (s.n_kv_heads * tiles * s.batch > kCounters) splits = 1;   // (far more workgroups than the chip holds)
   splits = splits < kMostSplits ? splits : kMostSplits;
   const Parts8 parts{(uint32_t*)ws, (float*)((char*)ws + BD_PAGED8_COUNTER_BYTES)};
-  const dim3 grid(splits, (unsigned)(s.n_kv_heads * tiles), s.batch);
-  // (more workgroups than compute units: the longest sequences first)
-  const int order = s.batch >= 2 && s.batch <= 64 && (long)splits * s.n_kv_heads * tiles * s.batch > 256 ? s.batch : 0;
+  // Ragged batches: where there are compute units for several splits of a sequence, those are dealt by length; where there are
+  // fewer units than sequences, the longest come first.
+  const long units = s.n_kv_heads * tiles;
+  const bool ragged = s.batch >= 2 && s.batch <= 64;
+  const int room = ragged && splits > 1 && units * s.batch <= 128 && s.max_pages >= 40 ? (int)(256 / units) : 0;
+  const int order = ragged && !room && units * s.batch > 256 ? s.batch : 0;
+  const dim3 grid(room ? room : splits, (unsigned)units, room ? 1 : s.batch);
 #define BD_RUN_N(D, C, E, N) \
-  hipLaunchKernelGGL((kv8_few_kernel<D, C, E, N>), grid, dim3(256), 0, st, BD_KV8_HOT_ARGS(s), splits, order, s, q, sc, parts, (uint16_t*)out)
+  hipLaunchKernelGGL((kv8_few_kernel<D, C, E, N>), grid, dim3(256), 0, st, BD_KV8_HOT_ARGS(s), splits, order, room, s, q, sc, parts, (uint16_t*)out)
 #define BD_RUN(D, C, E)                       \
   do {                                        \
     if (rows <= 16) BD_RUN_N(D, C, E, 1);     \

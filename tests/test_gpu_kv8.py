@@ -370,6 +370,47 @@ def test_a_long_context():
         p.attend((n,), window=9000, prefix=[1000], cap=50.0)
 
 
+@pytest.mark.parametrize("batch,hkv,tokens", [(2, 8, 1), (5, 2, 1), (16, 8, 1), (60, 1, 1), (64, 2, 2), (70, 1, 1), (40, 8, 1)])
+def test_ragged_batches_whose_splits_are_dealt_by_length(batch, hkv, tokens):
+    """Lengths from nothing to 6000 tokens in wide tables; more workgroups than compute units and fewer; rows of nobody."""
+    rng = np.random.default_rng(21)
+    lens = [int(6000 * rng.random() ** 3) for _ in range(batch)]
+    lens[0], lens[-1] = 6000, 0
+    kept = sorted({0, 1, batch // 2, batch - 1})   # (held against the oracle; the others have lengths alone)
+    p = Pair(batch, 2 * hkv, hkv, 64, "e4m3", "fp16", 48, seed=22)
+    for t in p.g.buffers[:2]:
+        t.zero_()
+    p.g.k_scales.view(torch.float32).fill_(1.0)
+    p.g.v_scales.view(torch.float32).fill_(1.0)
+    for t in p.g.buffers[4:]:
+        t.zero_()
+    p.append([n if b in kept else 0 for b, n in enumerate(lens)])
+    p.g.seq_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+    step = [tokens if b != 1 else 0 for b in range(batch)]
+    k = half(rng, "fp16", sum(step), hkv, 64)
+    v = half(rng, "fp16", sum(step), hkv, 64)
+    q = half(rng, "fp16", sum(step), 2 * hkv, 64).to(DEV)
+    cu = cu_of(step)
+    p.g.append(k.to(DEV), v.to(DEV), cu_tokens=cu, max_tokens=tokens)
+    outs = []
+    for splits in (None, 1, 2, 3, 7):
+        for window in (0, 900):
+            out = torch.full_like(q, 7.0)
+            p.g.attn(q, 0.125, out, cu_tokens=cu, max_tokens=tokens, window=window, num_splits=splits)
+            outs.append((window, f64(out)))
+    assert p.g.status.item() == 0
+    at = np.cumsum([0] + step)
+    for b in kept:
+        if step[b]:
+            rows = slice(at[b], at[b + 1])
+            p.o.lens[b] = lens[b]
+            p.o.append(b, f64(k[rows]), f64(v[rows]))
+            for window, got in outs:
+                want, spread, products, whole = O.attention(p.o, b, f64(q[rows]), lens[b], 0.125, window=window)
+                far = np.abs(got[rows] - want) - O.bar(want, spread, products, whole, 64, lens[b] + tokens, "fp16")
+                assert far.max() <= 0, (b, lens[b], window)
+
+
 def test_a_stream_of_its_own_and_two_at_once():
     """Two caches on two streams, steps of both under way at the same time."""
     pairs = [Pair(3, 8, 2, 128, "int8", "fp16", 5, seed=s) for s in (16, 17)]
