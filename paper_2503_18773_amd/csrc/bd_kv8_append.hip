@@ -99,22 +99,40 @@ __device__ __forceinline__ void store8(uint16_t* p, us8_t v) { *(us8_t*)p = v; }
 
 // The largest magnitude of a workgroup's values, given each thread's largest bit pattern (magnitudes of a half type order as
 // their bits do).
+template <int WAVES>
 __device__ __forceinline__ uint32_t group_max(uint32_t m, uint32_t* lds) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, d));
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
   __syncthreads();
-  return max(max(lds[0], lds[1]), max(lds[2], lds[3]));
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) m = max(m, lds[w]);
+  return m;
 }
 
-// code = x / scale to the nearest; both divisions as IEEE has them, so that the codes follow from the values alone
+// code = x / scale, the quotient rounded as IEEE division rounds it, so that the codes follow from the values alone, to the nearest.
+// q = x r with r = 1 / scale rounded correctly is within a step of the quotient, and q + (x - q scale) r then is the quotient rounded correctly
+// (Markstein's theorem; what the residue loses below 2^-149 is of quotients far below the smallest code).  Scales below 2^-90 are divided by.
+struct Divisor {
+  float scale, r;
+  __device__ __forceinline__ Divisor(float s) : scale(s), r(s >= 0x1p-90f ? 1.f / s : 0.f) {}
+  __device__ __forceinline__ float operator()(float x) const {
+    const float q = x * r;
+    return fmaf(fmaf(-q, scale, x), r, q);
+  }
+};
 template <int CODE>
-__device__ __forceinline__ uint32_t code4(const float* x, float scale) {
+__device__ __forceinline__ uint32_t code4(const float* x, const Divisor& by) {
   constexpr float kMost = CODE == BD_CODE_INT8 ? 127.f : 448.f;
   float y[4];
 #pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = by(x[e]);
+  if (by.r == 0.f) {   // (of the whole block)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = by.scale > 0.f ? x[e] / by.scale : 0.f;
+  }
+#pragma unroll
   for (int e = 0; e < 4; ++e) {
-    y[e] = scale > 0.f ? x[e] / scale : 0.f;
     if (CODE == BD_CODE_INT8) y[e] = rintf(y[e]);
     y[e] = fminf(fmaxf(y[e], -kMost), kMost);
   }
@@ -124,17 +142,19 @@ __device__ __forceinline__ uint32_t code4(const float* x, float scale) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
 }
 
-// Two kinds of workgroups.  blockIdx.x < row_groups: rows that stay in the element type, rotated queries and, if the step
-// completes no block of the sequence, keys and values on their way to the residual; a thread has one pair vector of up to
-// `heads` heads of a token.  The others: one block that the step completes, of one KV head's keys or values.  The first block of a sequence
-// takes its older tokens from the residual, and its workgroup files what the step leaves behind the last block there
-// afterwards: nobody else touches that head's residual.
+// Two kinds of workgroups.  The first 2 H * blocks, which take longest: one block that the step completes, of one KV head's keys or
+// values.  The first block of a sequence takes its older tokens from the residual, and its workgroup files what the step leaves behind
+// the last block there afterwards: nobody else touches that head's residual.  The others: rows that stay in the element type, rotated
+// queries and, if the step completes no block of the sequence, keys and values on their way to the residual; a thread has
+// one pair vector of up to `heads` heads of a token.
 template <int D, int CODE, int ELEM>
-__global__ __launch_bounds__(256) void kv8_append_kernel(Step8 s, Rows8 k, Rows8 v, Rows8 q, Rows8 q_out, Rotate8 rot, int row_groups,
-                                                         int heads, int blocks) {
+__global__ __launch_bounds__(4 * D) void kv8_append_kernel(BD_KV8_HOT_PARAMS, int heads, int blocks, Step8 s, Rows8 k, Rows8 v, Rows8 q, Rows8 q_out,
+                                                           Rotate8 rot) {
+  BD_KV8_HOT(s);
+  constexpr int kThreads = 4 * D;
   constexpr int kPairs = D / 16;
   constexpr float kMost = CODE == BD_CODE_INT8 ? 127.f : 448.f;
-  __shared__ uint32_t lds[4 + D * 33];
+  __shared__ uint32_t lds[8 + D * 33];
   const int b = blockIdx.y;
   Seq8 sq;
   if (!step_rows(s, b, sq)) return;
@@ -142,10 +162,11 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Step8 s, Rows8 k, Rows8
   const int H = s.n_kv_heads;
   const int r0 = sq.len % kBlock;
 
-  if ((int)blockIdx.x < row_groups) {
+  const int block_groups = 2 * H * blocks;
+  if ((int)blockIdx.x >= block_groups) {
     const int units = s.n_q_heads + 2 * H, groups = (units + heads - 1) / heads;
     const long tasks = (long)sq.n * groups * kPairs;
-    const long task = (long)blockIdx.x * 256 + threadIdx.x;
+    const long task = (long)((int)blockIdx.x - block_groups) * kThreads + threadIdx.x;
     if (task >= tasks) return;
     const int p = (int)(task % kPairs);
     const int g = (int)(task / kPairs % groups), i = (int)(task / ((long)kPairs * groups));
@@ -169,7 +190,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Step8 s, Rows8 k, Rows8
     return;
   }
 
-  const int rest = (int)blockIdx.x - row_groups, block = rest % blocks, unit = rest / blocks;   // unit: K heads, then V heads
+  const int block = (int)blockIdx.x % blocks, unit = (int)blockIdx.x / blocks;   // unit: K heads, then V heads
   if (block >= done) return;
   const bool is_v = unit >= H;
   const int h = is_v ? unit - H : unit;
@@ -182,12 +203,12 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Step8 s, Rows8 k, Rows8
 
   if (!is_v) {
     // keys: [token][channel], a thread's pair vectors; values at hand until the block's largest is known
-    constexpr int kTasks = kBlock * kPairs / 256;
+    constexpr int kTasks = kBlock * kPairs / kThreads;
     us8_t x[kTasks], y[kTasks];
     uint32_t most = 0;
 #pragma unroll
     for (int n = 0; n < kTasks; ++n) {
-      const int task = n * 256 + threadIdx.x, p = task % kPairs, i = t0 + task / kPairs;
+      const int task = n * kThreads + threadIdx.x, p = task % kPairs, i = t0 + task / kPairs;
       const PairVec at(rot, p);
       const uint16_t* row = i < 0 ? res + (size_t)(task / kPairs) * D : src + (sq.row + i) * from.token;
       x[n] = load8(row + 8 * at.a);
@@ -200,13 +221,14 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Step8 s, Rows8 k, Rows8
 #pragma unroll
       for (int e = 0; e < 8; ++e) most = max(most, max((uint32_t)x[n][e] & 0x7fffu, (uint32_t)y[n][e] & 0x7fffu));
     }
-    const float scale = to_f32<ELEM>((uint16_t)group_max(most, lds)) / kMost;
+    const float scale = to_f32<ELEM>((uint16_t)group_max<kThreads / 64>(most, lds)) / kMost;
+    const Divisor by(scale);
     if (page >= 0) {
       uint8_t* out = s.k_codes + ((size_t)page * H + h) * kBlock * D;
       if (threadIdx.x == 0) s.k_scales[(size_t)page * H + h] = scale;
 #pragma unroll
       for (int n = 0; n < kTasks; ++n) {
-        const int task = n * 256 + threadIdx.x;
+        const int task = n * kThreads + threadIdx.x;
         const PairVec at(rot, task % kPairs);
         float f[16];
 #pragma unroll
@@ -215,18 +237,18 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Step8 s, Rows8 k, Rows8
           f[8 + e] = to_f32<ELEM>(y[n][e]);
         }
         uint8_t* row = out + (size_t)(task / kPairs) * D;
-        *(u2_t*)(row + 8 * at.a) = u2_t{code4<CODE>(f, scale), code4<CODE>(f + 4, scale)};
-        *(u2_t*)(row + 8 * at.b) = u2_t{code4<CODE>(f + 8, scale), code4<CODE>(f + 12, scale)};
+        *(u2_t*)(row + 8 * at.a) = u2_t{code4<CODE>(f, by), code4<CODE>(f + 4, by)};
+        *(u2_t*)(row + 8 * at.b) = u2_t{code4<CODE>(f + 8, by), code4<CODE>(f + 12, by)};
       }
     }
   } else {
     // values: to [channel][token] through LDS, a word of four tokens' codes at a time
-    constexpr int kVecs = D / 8, kTasks = kBlock / 4 * kVecs / 256;
+    constexpr int kVecs = D / 8, kTasks = kBlock / 4 * kVecs / kThreads;
     us8_t x[kTasks][4];
     uint32_t most = 0;
 #pragma unroll
     for (int n = 0; n < kTasks; ++n) {
-      const int task = n * 256 + threadIdx.x, c = task % kVecs;
+      const int task = n * kThreads + threadIdx.x, c = task % kVecs;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int t = task / kVecs * 4 + j, i = t0 + t;
@@ -235,24 +257,25 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Step8 s, Rows8 k, Rows8
         for (int e = 0; e < 8; ++e) most = max(most, (uint32_t)x[n][j][e] & 0x7fffu);
       }
     }
-    const float scale = to_f32<ELEM>((uint16_t)group_max(most, lds)) / kMost;
+    const float scale = to_f32<ELEM>((uint16_t)group_max<kThreads / 64>(most, lds)) / kMost;
+    const Divisor by(scale);
     if (page >= 0) {
       uint8_t* out = s.v_codes + ((size_t)page * H + h) * kBlock * D;
       if (threadIdx.x == 0) s.v_scales[(size_t)page * H + h] = scale;
 #pragma unroll
       for (int n = 0; n < kTasks; ++n) {
-        const int task = n * 256 + threadIdx.x, c = task % kVecs;
+        const int task = n * kThreads + threadIdx.x, c = task % kVecs;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float f[4] = {to_f32<ELEM>(x[n][0][e]), to_f32<ELEM>(x[n][1][e]), to_f32<ELEM>(x[n][2][e]), to_f32<ELEM>(x[n][3][e])};
-          lds[4 + (8 * c + e) * 33 + task / kVecs] = code4<CODE>(f, scale);
+          lds[8 + (8 * c + e) * 33 + task / kVecs] = code4<CODE>(f, by);
         }
       }
       __syncthreads();
 #pragma unroll
-      for (int n = 0; n < D * 8 / 256; ++n) {
-        const int task = n * 256 + threadIdx.x;
-        const uint32_t* w = lds + 4 + (task / 8) * 33 + (task % 8) * 4;
+      for (int n = 0; n < D * 8 / kThreads; ++n) {
+        const int task = n * kThreads + threadIdx.x;
+        const uint32_t* w = lds + 8 + (task / 8) * 33 + (task % 8) * 4;
         *(u4_t*)(out + 16 * (size_t)task) = u4_t{w[0], w[1], w[2], w[3]};
       }
     }
@@ -261,7 +284,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Step8 s, Rows8 k, Rows8
 
   // (every thread's loads from the residual were used before the barrier in group_max)
   const int left = (int)(((unsigned)sq.len + (unsigned)sq.n) % kBlock);
-  for (int task = threadIdx.x; task < left * kPairs; task += 256) {
+  for (int task = threadIdx.x; task < left * kPairs; task += kThreads) {
     const int p = task % kPairs, t = task / kPairs, i = sq.n - left + t;
     const PairVec at(rot, p);
     const uint16_t* row = src + (sq.row + i) * from.token;
@@ -288,13 +311,16 @@ __global__ __launch_bounds__(256) void kv8_advance_kernel(Step8 s) {
 hipError_t launch_kv8_append(const Step8& s, int head_dim, int code, int elem, const Rows8& k, const Rows8& v, const Rows8& q,
                              const Rows8& q_out, const Rotate8& rot, hipStream_t st) {
   const int units = s.n_q_heads + 2 * s.n_kv_heads, pairs = head_dim / 16;
+  // Eight heads to a thread share a token's cosines and sines where there are threads enough (16384 tokens, 2 / 4 / 8 heads 101 / 90 / 88
+  // us, 9 prompts of up to 1333 56 / 50 / 50); a few tokens' heads are a thread's each.
   const int heads = (long)s.total * units * pairs > 256 * 2048 ? 8 : 1;
   const int groups = (units + heads - 1) / heads;
-  const long row_groups = ((long)s.max_tokens * groups * pairs + 255) / 256;
+  const int threads = 4 * head_dim;
+  const long row_groups = ((long)s.max_tokens * groups * pairs + threads - 1) / threads;
   const int blocks = (int)(((long)s.max_tokens + kBlock - 1) / kBlock);   // the most that a step of so many tokens completes
   const dim3 grid((unsigned)(row_groups + 2L * s.n_kv_heads * blocks), s.batch);
 #define BD_RUN(D, C, E) \
-  hipLaunchKernelGGL((kv8_append_kernel<D, C, E>), grid, dim3(256), 0, st, s, k, v, q, q_out, rot, (int)row_groups, heads, blocks)
+  hipLaunchKernelGGL((kv8_append_kernel<D, C, E>), grid, dim3(threads), 0, st, BD_KV8_HOT_ARGS(s), heads, blocks, s, k, v, q, q_out, rot)
 #define BD_RUN_TYPES(D)                                          \
   if (code == BD_CODE_INT8) {                                    \
     if (elem == BD_ELEM_F16) BD_RUN(D, BD_CODE_INT8, BD_ELEM_F16); \
