@@ -51,7 +51,7 @@ struct Scores8 {
 hipError_t launch_kv8_append(const Step8& s, int head_dim, int code, int elem, const Rows8& k, const Rows8& v, const Rows8& q,
                              const Rows8& q_out, const Rotate8& rot, hipStream_t st);
 hipError_t launch_kv8_advance(const Step8& s, hipStream_t st);
-hipError_t launch_kv8_attn(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, void* ws,
+hipError_t launch_kv8_attn(const Step8& s, bool few, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, void* ws,
                            void* out, hipStream_t st);
 int kv8_splits(const bd_paged8_cache* c, int max_tokens, int max_len);
 

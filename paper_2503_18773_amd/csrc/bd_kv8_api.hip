@@ -1,5 +1,6 @@
 // C-ABI entry points of the paged 8-bit cache: argument validation, launches, and the merge of splits.
 #include <algorithm>
+#include <cmath>
 
 #include "bd_kv8_part.h"
 
@@ -104,33 +105,43 @@ Step8 step_of(const bd_paged8_cache* c, const int32_t* cu, int32_t total, int32_
 
 Rows8 rows_of(const bd_rows* r) { return r ? Rows8{(uint16_t*)r->data, r->token_stride, r->head_stride} : Rows8{nullptr, 0, 0}; }
 
-// Up to how many rows (tokens times query heads) of a KV head go by 16 or 32 against a block in a wave's registers, each tile reading the
-// cache for itself; more are tiles of many_rows() that share blocks in LDS.
-constexpr long kFewRows = 64;
+// Which kernel a call of up to `rows` rows (tokens times query heads) of a KV head takes: tiles of 16 or 32 rows whose waves have
+// blocks of their own (launch_kv8_few), or tiles of many_rows() whose waves share blocks (launch_kv8_many).  The latter do twice as much with a
+// block's codes, but leave compute units idle that the former's tiles, or splits of those, would fill:
+// - up to 64 rows, and up to 256 where two splits of each tile find units (8 KV heads, behind 8192 tokens: 64 tokens of one sequence 36 us against
+//   50, 17 of four 44 / 49; 64 of four, 256 tiles, 72 / 55);
+// - one split, which is what kv8_splits chooses for short sequences, and one round and a half of tiles (prompts, one split: 1000 tokens of 2 KV heads, 250
+//   tiles, 17 / 38; 256 of 8 KV heads, 256 tiles, 12 / 17.5; 100 of four sequences, 416 tiles, 13.4 / 15; 600 of 8 KV heads, 600 tiles, 31.6 / 29.6).
+bool takes_few(const bd_paged8_cache* c, long rows, int num_splits) {
+  const long tiles = (long)c->batch * c->n_kv_heads * few_tiles(rows);
+  return rows <= 64 || (rows <= 256 && tiles <= 128) || (num_splits == 1 && tiles <= 448);
+}
 
 }  // namespace
 
-bool kv8_few(long rows) { return rows <= kFewRows; }
-
 // Few rows: one workgroup on a compute unit at most (it asks for as much as the unit can draw; 32 splits of 8 KV heads at 128K
-// tokens 57 us, 64 splits 73), and of those two blocks in each where there are many, since a split costs its merge 0.08 us (4095
-// tokens, 8 units, 8 / 16 / 32 splits 12.7 / 11.6 / 14.3 us; 2047 tokens 4 / 8 / 16 splits 12.1 / 10.4 / 11.1; one unit, 60000 tokens 32 /
-// 64 / 128 splits 24.9 / 21.7 / 24.4).  Up to four blocks are a wave's each in one workgroup, which spares the merge.
+// tokens 57 us, 64 splits 73).  Of those, a split takes some 0.6 us off for each of its blocks that it shares out, and costs its merge 0.02 us for each
+// row: sqrt(30 blocks / rows) is best (4 rows, 8 units: 4095 tokens, 8 / 16 / 32 splits 12.7 / 11.6 / 14.3 us; 2047 tokens 4 / 8 / 16 splits
+// 12.1 / 10.4 / 11.1; one unit, 60000 tokens 32 / 64 / 128 splits 24.9 / 21.7 / 24.4; 24 rows, one unit, 16000 tokens 62 splits 48.5, 13 splits 32.6).
+// Up to four blocks are a wave's each in one workgroup, which spares the merge.
+// Many rows: as many workgroups as compute units hold (of head dimension 64 two, of 128 one), eight blocks in each at least.
 int kv8_splits(const bd_paged8_cache* c, int max_tokens, int max_len) {
   const long rows = (long)max_tokens * (c->n_q_heads / c->n_kv_heads);
   const long blocks = (std::max(max_len, 1) - 1L) / kBlock + 1;
-  if (kv8_few(rows)) {
-    const long units = (long)c->batch * c->n_kv_heads * few_tiles(rows);
-    const long want = blocks <= 4 ? 1 : blocks <= 8 ? blocks : std::min(std::max(8L, blocks / 2), 64L);
-    return (int)std::max(1L, std::min(want, 256 / units));
+  if (takes_few(c, rows, blocks <= 24 ? 1 : 2)) {
+    const long held = std::min(rows, few_rows(rows)), units = (long)c->batch * c->n_kv_heads * few_tiles(rows);
+    const long want = blocks <= 4 ? 1 : std::min((long)std::lround(std::sqrt(30. * blocks / held)), blocks);
+    const long splits = std::max(1L, std::min(want, 256 / units));
+    if (splits == 1 || takes_few(c, rows, 2)) return (int)splits;
+    return 1;
   }
   const long units = (long)c->batch * c->n_kv_heads * ((rows + many_rows(c->head_dim) - 1) / many_rows(c->head_dim));
-  return (int)std::max(1L, std::min((blocks + 7) / 8, 256 / units));
+  return (int)std::max(1L, std::min((blocks + 7) / 8, (c->head_dim == 64 ? 512 : 256) / units));
 }
 
-hipError_t launch_kv8_attn(const Step8& s, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, void* ws,
+hipError_t launch_kv8_attn(const Step8& s, bool few, int head_dim, int code, int elem, const Rows8& q, const Scores8& sc, int splits, void* ws,
                            void* out, hipStream_t st) {
-  if (kv8_few((long)s.max_tokens * s.gq)) return launch_kv8_few(s, head_dim, code, elem, q, sc, splits, ws, out, st);
+  if (few) return launch_kv8_few(s, head_dim, code, elem, q, sc, splits, ws, out, st);
   float* part = (float*)((char*)ws + BD_PAGED8_COUNTER_BYTES);
   const hipError_t e = launch_kv8_many(s, head_dim, code, elem, q, sc, splits, part, out, st);
   if (e != hipSuccess || splits == 1) return e;
@@ -204,8 +215,8 @@ size_t bd_paged8_workspace_bytes(const bd_paged8_cache* c, int32_t total, int32_
     return std::max((size_t)std::min(num_splits, kMostSplits) * c->batch * c->n_kv_heads * few_tiles(rows), c->batch > 1 ? (size_t)256 : 0) * std::min(rows, few_rows(rows));
   };
   const long rows = std::min(max_tokens, total) * gq;
-  size_t filed = kv8_few(rows) ? few(rows) : (size_t)num_splits * total * c->n_q_heads;
-  if (kv8_few(gq)) filed = std::max(filed, few(gq));   // (a call without cu_tokens, whatever its max_tokens)
+  size_t filed = takes_few(c, rows, num_splits) ? few(rows) : (size_t)num_splits * total * c->n_q_heads;
+  if (takes_few(c, gq, num_splits)) filed = std::max(filed, few(gq));   // (a call without cu_tokens, whatever its max_tokens)
   return BD_PAGED8_COUNTER_BYTES + filed * (c->head_dim + 2) * sizeof(float);
 }
 
@@ -222,12 +233,13 @@ bd_status bd_paged8_attn(const bd_paged8_cache* c, const bd_rows* q, const int32
   if (!aligned(out, 16) || !aligned(workspace, 16)) return BD_ERR_ALIGNMENT;
   const Step8 st = step_of(c, cu_tokens, total, max_tokens);
   const long rows = (long)st.max_tokens * st.gq;
+  const bool few = takes_few(c, rows, num_splits);
   // launch grid dimensions: KV heads x tiles of rows, tiles x splits; the merge's rows
-  if (num_splits > 65535 || (kv8_few(rows) ? few_tiles(rows) * c->n_kv_heads : (rows + many_rows(c->head_dim) - 1) / many_rows(c->head_dim) * num_splits) > 65535 ||
+  if (num_splits > 65535 || (few ? few_tiles(rows) * c->n_kv_heads : (rows + many_rows(c->head_dim) - 1) / many_rows(c->head_dim) * num_splits) > 65535 ||
       ((long)st.max_tokens * c->n_q_heads + 3) / 4 > (1L << 24) - 1)
     return BD_ERR_UNSUPPORTED;
   const Scores8 sc{scores->softmax_scale, scores->softcap, scores->slopes, scores->prefix_lens, scores->window};
-  return hip_status(launch_kv8_attn(st, c->head_dim, c->code_type, c->elem_type, rows_of(q), sc, num_splits, workspace, out,
+  return hip_status(launch_kv8_attn(st, few, c->head_dim, c->code_type, c->elem_type, rows_of(q), sc, num_splits, workspace, out,
                                     (hipStream_t)stream));
 }
 

@@ -61,7 +61,7 @@ __device__ __forceinline__ void get2(const float* p, float& a, float& b) {
 __device__ __forceinline__ float merge_weight(float m, float top) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top); }
 
 // A ragged batch's workgroups, dealt by length: of the `room` that there are for a head's tile, a sequence gets one for so many blocks each
-// (six at least) that all of them find room.  This workgroup's sequence, its number among that one's, how many those are, and the first one's
+// (six at least, and no more than twice `splits` in all) that all of them find room.  This workgroup's sequence, its number among that one's, how many those are, and the first one's
 // number; false: it is left over.  (Lengths as they are before the step, whatever lists and prefixes make of them.)  Against as many splits for
 // each: 4 sequences of 20000 down to 6700 tokens 31.8 -> 28.6 us, 3 of up to 60000 60.5 -> 52.0, 24 of up to 5000 and 4 KV heads 27.0 -> 22.8; it
 // takes a microsecond, which short ones do not make up for (16 of up to 4000, five queries each, 34.3 / 35.8, 2 of 700 9.6 / 10.6): the
@@ -69,13 +69,13 @@ __device__ __forceinline__ float merge_weight(float m, float top) { return m == 
 struct Share {
   int b, split, splits, first;
 };
-__device__ __forceinline__ bool fair_share(const Step8& s, int lane, int room, int window, Share& share) {
+__device__ __forceinline__ bool fair_share(const Step8& s, int lane, int room, int most, int window, Share& share) {
   int blocks = lane < s.batch ? max(s.seq_lens[lane], 0) / kBlock + 1 : 0;
   if (window) blocks = min(blocks, window / kBlock + 2);
   const float mine = (float)blocks;
   float each = ceilf(fmaxf(join_groups(row_sum16(mine), Add()) / (float)max(1, room - s.batch / 2), 6.f)), wanted;
   for (int i = 0;; ++i) {
-    wanted = fminf(ceilf(mine / each), (float)kMostSplits);
+    wanted = fminf(ceilf(mine / each), (float)most);
     const float need = join_groups(row_sum16(wanted), Add());
     if (need <= (float)room) break;
     if (i == 8) {   // (not seen; one for each has room: launch_kv8_few)
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256, 1) void kv8_few_kernel(BD_KV8_HOT_PARAMS, int 
   int b, split = blockIdx.x, slot = 0;   // slot: where the sequence's partial results begin, of its head's tile
   if (room) {
     Share share;
-    if (!fair_share(s, lane, room, sc.window, share)) return;
+    if (!fair_share(s, lane, room, min(2 * splits, kMostSplits), sc.window, share)) return;
     b = share.b;
     split = share.split;
     splits = share.splits;
