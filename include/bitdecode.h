@@ -64,7 +64,7 @@ extern "C" {
 typedef enum {
   BD_OK = 0,
   BD_ERR_INVALID_ARG = -1,   /* NULL pointer, non-positive size, bad enum, bad length */
-  BD_ERR_UNSUPPORTED = -2,   /* a shape this build has no kernel for (head_dim != 128; batch, KV heads times pieces of the query group, or batch times KV heads, beyond 65535, a launch grid dimension) */
+  BD_ERR_UNSUPPORTED = -2,   /* a shape this build has no kernel for (head_dim != 128; batch, KV heads times pieces of the query group, or batch times KV heads, beyond 65535, a launch grid dimension; bd_paged8_*: likewise, or a softcap beyond 1024) */
   BD_ERR_ALIGNMENT = -3,     /* a device pointer is not 16-byte aligned */
   BD_ERR_CAPACITY = -4,      /* the cache cannot hold the tokens asked for */
   BD_ERR_HIP = -5            /* a HIP runtime call failed; see bd_last_hip_error() */
@@ -413,7 +413,7 @@ typedef struct bd_rotation {
  * (window 0: all of them).  A query that sees nothing gives zeros. */
 typedef struct bd_scores {
   float softmax_scale;
-  float softcap;               /* 0: none */
+  float softcap;               /* 0: none; at most 1024 */
   const float* slopes;         /* device fp32 [n_q_heads], may be NULL */
   const int32_t* prefix_lens;  /* device [B], may be NULL; one that is longer than the sequence ends with it */
   int32_t window;
@@ -440,7 +440,8 @@ size_t bd_paged8_workspace_bytes(const bd_paged8_cache* c, int32_t total, int32_
 
 /* Attention of the step's queries over the cache, after bd_paged8_append has filed the step's tokens: out (device, 16-byte aligned,
  * [total][n_q_heads][D]) = softmax(scores) V for each row and head; query head h reads KV head h / (n_q_heads / n_kv_heads).
- * Any num_splits >= 1 gives the same up to the rounding of fp32 sums; workspace: 16-byte aligned, may be NULL for one split. */
+ * Any num_splits >= 1 gives the same up to the rounding of fp32 sums (some calls take fewer
+ * or share them out by length); workspace: 16-byte aligned, may be NULL for one split.  `out` is no part of another argument's memory. */
 bd_status bd_paged8_attn(const bd_paged8_cache* c, const bd_rows* q, const int32_t* cu_tokens, int32_t total, int32_t max_tokens,
                          const bd_scores* scores, int32_t num_splits, void* workspace, void* out, void* stream);
 

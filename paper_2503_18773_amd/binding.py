@@ -170,6 +170,17 @@ def _stream(stream):
     return _raw_stream()
 
 
+def _stream_on(stream, device: int):
+    """As _stream, for calls whose memory is on the device of that number (-1: the host's, of descriptions alone): the library launches on the
+    current one."""
+    if device >= 0:
+        import torch
+        current = torch.cuda.current_device()
+        if current != device:
+            raise ValueError(f"the cache is on device {device}, the current device is {current}: use torch.cuda.device({device})")
+    return _stream(stream)
+
+
 class _CtypesCall:
     """The functions of csrc/bd_call.c, for where it has not been built."""
 
@@ -664,7 +675,7 @@ class PagedKV8Cache:
             if rotation.device != self._layout[7]:
                 raise ValueError(f"rotation: on {self._layout[8]}")
         _check(_call.append8(_address("bd_paged8_append"), self.desc, self._layout, k_new, v_new, q, q_out, cu_tokens, max_tokens, desc,
-                             positions, _stream(stream)), "bd_paged8_append")
+                             positions, _stream_on(stream, self._layout[7])), "bd_paged8_append")
         return q_out
 
     def workspace(self, rows: int, max_tokens: int, max_len: int, num_splits: int):
@@ -685,12 +696,13 @@ class PagedKV8Cache:
         the step's among them, which num_splits is chosen for (any value gives the same result)."""
         num_splits, ws = self.workspace(len(q), max_tokens, self.max_len if max_len is None else max_len, num_splits or 0)
         _check(_call.attn8(_address("bd_paged8_attn"), self.desc, self._layout, q, cu_tokens, max_tokens, softmax_scale, softcap, slopes,
-                           prefix_lens, window, num_splits, ws, out, _stream(stream)), "bd_paged8_attn")
+                           prefix_lens, window, num_splits, ws, out, _stream_on(stream, self._layout[7])), "bd_paged8_attn")
         return out
 
     def advance(self, cu_tokens=None, rows: int | None = None, max_tokens: int = 1, stream=None):
         """Counts the step's tokens into seq_lens.  rows: of the step's tensors (of one token a sequence, the batch)."""
         _CtypesCall._list_of(cu_tokens, self._layout, self.desc.batch + 1, self._layout[5], "cu_tokens")
+        _stream_on(stream, self._layout[7])
         bd_paged8_advance(self.desc, cu_tokens, self.desc.batch if rows is None else rows, max_tokens, stream)
 
     def host_buffer(self, i: int):

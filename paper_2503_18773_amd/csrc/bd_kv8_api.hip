@@ -195,8 +195,8 @@ bd_status bd_paged8_append(const bd_paged8_cache* c, const bd_rows* k_new, const
   if (q && ((s = check_rows(q)) != BD_OK || (s = check_rows(q_out)) != BD_OK)) return s;
   if (q && (q_out->token_stride < c->head_dim || q_out->head_stride < c->head_dim)) return BD_ERR_INVALID_ARG;   // rows on top of each other
   const Step8 st = step_of(c, cu_tokens, total, max_tokens);
-  // workgroups of a launch: fewer than 2^32 threads
-  if (((long)st.max_tokens * (c->n_q_heads + 2 * c->n_kv_heads) * (c->head_dim / 16) + 255) / 256 + 2L * c->n_kv_heads * ((st.max_tokens - 1L) / kBlock + 1) > (1L << 24) - 1)
+  // a launch's threads, of which up to 512 are a workgroup: fewer than 2^32
+  if (((long)st.max_tokens * (c->n_q_heads + 2 * c->n_kv_heads) * (c->head_dim / 16) + 255) / 256 + 2L * c->n_kv_heads * ((st.max_tokens - 1L) / kBlock + 1) > (1L << 23) - 1)
     return BD_ERR_UNSUPPORTED;
   return hip_status(launch_kv8_append(st, c->head_dim, c->code_type, c->elem_type, rows_of(k_new), rows_of(v_new), rows_of(q), rows_of(q_out),
                                       r, (hipStream_t)stream));
@@ -226,6 +226,7 @@ bd_status bd_paged8_attn(const bd_paged8_cache* c, const bd_rows* q, const int32
   if (s != BD_OK) return s;
   if ((s = check_buffers8(c)) != BD_OK || (s = check_step(c, cu_tokens, total, max_tokens)) != BD_OK) return s;
   if (!scores || num_splits < 1 || scores->window < 0 || !(scores->softcap >= 0.f)) return BD_ERR_INVALID_ARG;
+  if (scores->softcap > 1024.f) return BD_ERR_UNSUPPORTED;
   if (!aligned(scores->slopes, 4) || !aligned(scores->prefix_lens, 4)) return BD_ERR_ALIGNMENT;
   if (total == 0) return BD_OK;
   if ((s = check_rows(q)) != BD_OK) return s;

@@ -165,11 +165,10 @@ __global__ __launch_bounds__(4 * D) void kv8_append_kernel(BD_KV8_HOT_PARAMS, in
   const int block_groups = 2 * H * blocks;
   if ((int)blockIdx.x >= block_groups) {
     const int units = s.n_q_heads + 2 * H, groups = (units + heads - 1) / heads;
-    const long tasks = (long)sq.n * groups * kPairs;
-    const long task = (long)((int)blockIdx.x - block_groups) * kThreads + threadIdx.x;
-    if (task >= tasks) return;
-    const int p = (int)(task % kPairs);
-    const int g = (int)(task / kPairs % groups), i = (int)(task / ((long)kPairs * groups));
+    const uint32_t task = (blockIdx.x - block_groups) * kThreads + threadIdx.x;   // (fewer than 2^32: bd_paged8_append)
+    const int p = task % kPairs;
+    const int g = (int)(task / kPairs % groups), i = (int)(task / kPairs / groups);
+    if (i >= sq.n) return;
     const int row = sq.row + i;
     const PairVec at(rot, p);
     Angles w;

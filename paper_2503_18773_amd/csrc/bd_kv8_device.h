@@ -104,13 +104,14 @@ struct Linear {
 
 // N x 4 (or 16) products of a row to scores, -infinity for tokens that the row does not see.  c >= 0: what a product is worth, in natural
 // units; from + offset(t, i): the token.  Every pass is decided on once for all of them.
-// The cap: cap tanh(y) = cap + 2 cap r with r = -1 / (1 + e^2y), within 2^-23 of it absolutely, which is what a score needs.
+// The cap: cap tanh(y) = cap + 2 cap r with r = -1 / (1 + e^2y), r within 2^-23 absolutely: the score within 2^-22 cap, which for caps of up to 1024
+// (bd_paged8_attn takes no larger ones) is less than what rounding a weight to 11 bits is.
 template <class X, int N, class Offset>
 __device__ __forceinline__ Linear finish_scores(X* x, float c, const Scores8& sc, const RowView& view, bool masked, int from, Offset offset) {
   constexpr int K = sizeof(X) / 4;
   Linear f{fmaxf(c * kLog2e, 1e-30f), 0.f};   // (0 times -infinity is no score)
   if (sc.cap > 0.f) {
-    const float twice = 2.f * kLog2e * c / sc.cap;
+    const float twice = fminf(2.f * kLog2e * c / sc.cap, 1e30f);   // (nor is 0 times infinity)
 #pragma unroll
     for (int t = 0; t < N; ++t)
 #pragma unroll

@@ -151,6 +151,7 @@ def test_what_is_refused_before_anything_is_launched():
     assert attn(q=None) == attn(out=None) == attn(scores=False) == attn(splits=0) == attn(splits=2) == attn(window=-1) == -1
     assert attn(cap=-1.0) == attn(cap=float("nan")) == attn(cu=None, total=5) == attn(total=-2) == attn(most=0) == -1
     assert attn(out=4100) == attn(splits=2, ws=4104) == attn(slopes=4098) == attn(prefix=4098) == attn(q=rows(4096, 8, 12)) == -3
+    assert attn(cap=1025.0) == -2
     assert attn(splits=65536, ws=4096) == attn(total=2 ** 31 - 1, most=2 ** 31 - 1) == -2
     assert attn(total=0, q=None, out=None) == 0
     assert L.bd_paged8_advance(ctypes.byref(c), None, 3, 1, None) == L.bd_paged8_advance(None, 4096, 3, 1, None) == -1
@@ -181,6 +182,15 @@ def test_the_class_checks_its_tensors(call, monkeypatch):
                 lambda: B.PagedKV8Cache(2, 4, 2, "int8", 6, [[0], [1]], device="cpu", buffers=[torch.zeros(4)] * 6)):
         with pytest.raises(ValueError):
             bad()
+    # memory on another device than the current one (named by its number; there need not be one here)
+    c._layout = c._layout[:7] + (3,) + c._layout[8:]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="current device is 0"):
+        c.advance(stream=stream)
+    with pytest.raises(ValueError, match="current device is 0"):
+        B._stream_on(stream, 3)
+    assert B._stream_on(stream, 0) == B._stream_on(stream, -1) == 0
+    c._layout = c._layout[:7] + (-1,) + c._layout[8:]
     with pytest.raises(B.BitDecodeError):
         B.PagedKV8Cache(2, 4, 3, "int8", 6, [[0], [1]], device="cpu")
     with pytest.raises(B.BitDecodeError):
