@@ -626,7 +626,8 @@ class PagedKV8Cache:
     torch tensors (zero-filled, or `buffers`, the caller's own: k_codes, v_codes, k_scales, v_scales, k_res, v_res), and the block
     table and the lengths, which the caller owns and layers may share.  A step is append (keys and values, rotated on the way), attn
     (any number of times) and, once for all layers that share the lengths, advance; cu_tokens (int32 [batch + 1]) says which rows of a step's
-    tensors are whose, None: row b is the one token of sequence b.  Every operation is a call into the library."""
+    tensors are whose, None: row b is the one token of sequence b.  Every operation is a call into the library.  A cache has one
+    workspace: its calls are ordered, by one stream or by events; a call that is to be captured runs once before."""
 
     def __init__(self, batch: int, n_q_heads: int, n_kv_heads: int, code: str, num_pages: int, block_table, head_dim: int = 128,
                  dtype=None, seq_lens=None, buffers=None, device="cuda:0"):
@@ -680,14 +681,21 @@ class PagedKV8Cache:
 
     def workspace(self, rows: int, max_tokens: int, max_len: int, num_splits: int):
         """The splits of a call (num_splits; 0: chosen for max_len) and a workspace for it, None for one split.  As KVCache.workspace
-        it grows only, and outgrown buffers stay alive."""
+        it grows only, and outgrown buffers stay alive.  Its counters are zeros before any stream's call: growing waits for that, and is
+        refused while a graph is captured."""
         num_splits, need = _call.plan8(_address("bd_paged8_choose_splits"), _address("bd_paged8_workspace_bytes"), self.desc, rows, max_tokens,
                                        max_len, num_splits)
         if need > self._ws_bytes:
             import torch
+            on_gpu = self._layout[7] >= 0
+            if on_gpu and torch.cuda.is_current_stream_capturing():   # (the graph would hold the zeros that calls outside of it need)
+                raise ValueError("the workspace has to grow: run the call once before it is captured")
+            ws = torch.zeros(need, dtype=torch.uint8, device=self.device)
+            if on_gpu:   # (filled on the current stream, which need not be the call's)
+                torch.cuda.current_stream(self.device).synchronize()
             if self._ws is not None:
                 self._retired.append(self._ws)
-            self._ws, self._ws_bytes = torch.zeros(need, dtype=torch.uint8, device=self.device), need
+            self._ws, self._ws_bytes = ws, need
         return num_splits, self._ws if need else None
 
     def attn(self, q, softmax_scale: float, out, cu_tokens=None, max_tokens: int = 1, max_len: int | None = None, softcap: float = 0.0,

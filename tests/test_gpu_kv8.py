@@ -437,6 +437,51 @@ def test_a_stream_of_its_own_and_two_at_once():
         assert torch.equal(one, two)
 
 
+def test_the_first_call_may_be_another_streams():
+    """The workspace's counters are zeros for it, over memory that was not, whatever is under way on the current stream."""
+    p, like = (Pair(3, 8, 2, 128, "int8", "fp16", 5, seed=21) for _ in range(2))
+    for x in (p, like):
+        x.append((300, 400, 500))
+        x.append((1, 1, 1), advance=False)
+    q = half(p.rng, "fp16", 3, 8, 128).to(DEV)
+    want, got = torch.empty_like(q), torch.empty_like(q)
+    like.g.attn(q, 0.1, want, num_splits=3)
+    _, ws = like.g.workspace(3, 1, like.g.max_len, 3)
+    other, x = torch.cuda.Stream(), torch.ones(4096, 4096, device=DEV)
+    used = torch.full_like(ws, 255)
+    torch.cuda.synchronize()
+    del used
+    for _ in range(20):
+        y = x @ x
+    p.g.attn(q, 0.1, got, num_splits=3, stream=other)
+    torch.cuda.synchronize()
+    assert y[0, 0].item() == 4096 and torch.equal(want, got)
+
+
+def test_a_workspace_does_not_grow_inside_of_a_capture():
+    p = Pair(2, 8, 2, 128, "e4m3", "bf16", 5, seed=22)
+    p.append((300, 600))
+    p.append((1, 1), advance=False)
+    q = half(p.rng, "bf16", 2, 8, 128).to(DEV)
+    want, got = torch.empty_like(q), torch.zeros_like(q)
+    for ready in (False, True):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got.zero_()
+            if ready:
+                p.g.attn(q, 0.1, got, num_splits=3)
+            else:
+                with pytest.raises(ValueError, match="before it is captured"):
+                    p.g.attn(q, 0.1, got, num_splits=3)
+        p.g.attn(q, 0.1, want, num_splits=3)
+    for _ in range(3):
+        graph.replay()
+        p.g.attn(q, 0.1, want, num_splits=3)
+        torch.cuda.synchronize()
+        assert torch.equal(want, got) and want.abs().max().item() > 0
+        got.zero_()
+
+
 def test_decoding_in_a_graph():
     """Two layers that share table and lengths: a step captured once and replayed over a block's end, the program's own work between
     the replays, against the same steps one by one."""
