@@ -298,6 +298,23 @@ def test_prompts_and_pieces_of_prompts(code, dtype, dim, splits):
     assert p.g.status.item() == 0
 
 
+@pytest.mark.parametrize("splits", [None, 1])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+def test_prompts_in_one_split_of_large_tiles(code, dtype, dim, splits):
+    """More small tiles (4 sequences, 8 heads, 15 tiles of 32 rows: 480) than a call of one split is given: large ones write the outputs themselves."""
+    p = Pair(4, 8, 8, dim, code, dtype, 8, seed=23)
+    p.append((0, 300, 128, 512))
+    counts = (460, 0, 129, 333)
+    p.append(counts, advance=False)
+    p.attend(counts, splits=splits, start=5, behind=9)
+    p.attend(counts, splits=splits, cap=3.0, scale=-0.2)
+    p.attend(counts, splits=splits, window=130, slopes=[0.1, 0.02, 0.5, -0.01, 0.0, 1.0, 0.3, 0.004])
+    p.attend(counts, splits=splits, prefix=[150, 0, 1000, 5], window=40)
+    assert p.g.status.item() == 0
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.125, 1.0, 3.0])
 def test_scales_of_any_sign_and_peaked_weights(scale):
     p = Pair(2, 4, 2, 64, "int8", "fp16", 5, seed=11)
