@@ -16,7 +16,7 @@
  *  - For bd_cache, lengths are host integers and are uniform across the batch (the paper's
  *    "Batches" setting, Sec. V-A: same length, padded); bd_paged_cache (further down) keeps
  *    per-sequence lengths on the device (the "Page" setting).
- *  - head_dim is 128.  The residual block N_r (Eq. 1) is 128 tokens for every integer format; the
+ *  - head_dim is 128 (bd_paged8_cache: 64 or 128).  The residual block N_r (Eq. 1) is 128 tokens for every integer format; the
  *    quantization group is 128 as well, except for the _G64 / _G32 formats (64 / 32, with K
  *    channel-wise or, _KT_G64 / _KT_G32, per token); the MX group is 32 for BD_FMT_MXFP4, which
  *    keeps no residual.

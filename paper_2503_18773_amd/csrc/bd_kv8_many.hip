@@ -356,7 +356,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void kv8_many_kernel(Step8 s, Rows8 
 // 748, unphased with a barrier a block 666; 1024 tokens behind 31744, a window and a cap 354 / 437 / 387.
 // 64: half the products to as many weights, so that there is less to put beside them: four waves, unphased, two workgroups on a unit.  Six prompts of up to 1333
 // tokens, 16 heads and a bias 37 us, eight waves in phases 49 (unphased 40 against 31 without a bias); only a long prompt is better off with those, 8192
-// tokens 457 / 430.  (Kernel times after a pause; 8192 tokens of head dimension 128 in a row of passes: 527 us, 1.04 PFLOP/s.)
+// tokens 457 / 430.  (Kernel times after a pause; 8192 tokens of head dimension 128 in a row of passes: 527 to 538 us, 1.02 to 1.04 PFLOP/s.)
 template <int D, int CODE, int ELEM>
 void run(const Step8& s, const Rows8& q, const Scores8& sc, int splits, float* part, void* out, hipStream_t st) {
   constexpr int kWaves = many_rows(D) / 32;
